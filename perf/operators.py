@@ -1,0 +1,231 @@
+"""Performance cases of the fully-connected operators: the 8-bit product and the mixture-of-experts layer.
+
+Both are what a program runs behind its feature maps, on one row per video stream, or (the product) on one row per pixel:
+
+* ``fc``   ``dc_fc_i8_layer``: rows in fp32 or bf16 are rounded to 8-bit integers with a scale of their own, multiplied with
+           8-bit weights (a scale per output channel) and scaled back; bias and ReLU as in ``dc_fc_layer``.
+* ``moe``  ``dc_moe_layer``: a router picks ``top_k`` of ``experts`` pairs of fully-connected layers for every row and adds
+           their outputs, weighted by the router's softmax.  Weights in the rows' type or in 8 bits with a scale per channel.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+own = False
+DEVICE = "cuda:0"
+_TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def _fc(name, rows, k, cout, dtype, relu=True):
+    return dict(name=name, kind="fc", rows=rows, k=k, cout=cout, dtype=dtype, relu=relu)
+
+
+def _moe(name, tokens, experts, top_k, cin, hidden, cout, dtype, wtype, act="gated", renormalize=True):
+    return dict(name=name, kind="moe", tokens=tokens, experts=experts, top_k=top_k, cin=cin, hidden=hidden, cout=cout, dtype=dtype,
+                wtype=wtype, act=act, renormalize=renormalize)
+
+
+def listed():
+    return [
+        # the first fully-connected layer of the steering network, one camera: launches are everything
+        _fc("fc 1152->100 bf16 x1", 1, 1152, 100, "bf16"),
+        # the first layer of the AlexNet-style head, one stream in single precision: its weights through memory
+        _fc("fc 9216->4096 f32 x1", 1, 9216, 4096, "f32"),
+        # the same for the 64 streams of batched serving
+        _fc("fc 9216->4096 bf16 x64", 64, 9216, 4096, "bf16"),
+        # a camera hub whose sizes divide by nothing
+        _fc("fc 1023->517 f32 x37", 37, 1023, 517, "f32", relu=False),
+        # a 1x1 layer over the pixels of 64 maps of 14x14
+        _fc("fc 1024->256 bf16 x12544", 12544, 1024, 256, "bf16"),
+        # a wide product over many rows, the largest: the matrix units
+        _fc("fc 4096->4096 bf16 x16384", 16384, 4096, 4096, "bf16", relu=False),
+        # one stream through a small layer with one expert a row
+        _moe("moe 8of1 256 f32 x1", 1, 8, 1, 256, 512, 256, "f32", "f32", act="relu", renormalize=False),
+        # one stream, gated experts of ordinary width: two experts' weights through memory
+        _moe("moe 8of2 2048 bf16 x1", 1, 8, 2, 2048, 4096, 2048, "bf16", "bf16"),
+        # five streams, ragged sizes, 8-bit weights
+        _moe("moe 6of2 1000 bf16 i8 x5", 5, 6, 2, 1000, 1411, 777, "bf16", "i8"),
+        # 16 streams in single precision
+        _moe("moe 8of2 1024 f32 x16", 16, 8, 2, 1024, 2048, 1024, "f32", "f32", act="relu"),
+        # 64 streams, many small experts: nearly every expert has rows, few each
+        _moe("moe 32of4 2048 bf16 x64", 64, 32, 4, 2048, 1024, 2048, "bf16", "bf16"),
+        # 64 streams, few large experts in 8 bits, the largest of this kind: 16 rows an expert
+        _moe("moe 8of2 4096 bf16 i8 x64", 64, 8, 2, 4096, 8192, 4096, "bf16", "i8"),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _matrices(case):
+    return 3 if case["act"] == "gated" else 2
+
+
+def draw(rng):
+    """A case of the same ranges: rows from one to many thousands, whole and odd sizes, every type."""
+    def size(lo, hi):
+        v = _log_uniform(rng, lo, hi)
+        return max(lo, v // 64 * 64) if v >= 64 and rng.random() < 0.5 else v
+    if rng.random() < 0.5:
+        case = dict(kind="fc", rows=rng.choice([1, _log_uniform(rng, 1, 64), _log_uniform(rng, 1, 64), _log_uniform(rng, 64, 16384)]),
+                    k=size(64, 25088), cout=size(16, 4096), dtype=rng.choice(["bf16", "bf16", "f32"]), relu=rng.random() < 0.5)
+        while case["rows"] * case["k"] * case["cout"] > 16384 * 4096 * 4096 or case["rows"] * case["k"] > 16384 * 4096:
+            case["rows"] = max(1, case["rows"] // 2)
+        return case
+    experts = rng.choice([4, 6, 8, 16, 32, 64])
+    dtype = rng.choice(["bf16", "bf16", "f32"])
+    case = dict(kind="moe", tokens=rng.choice([1, _log_uniform(rng, 1, 64), _log_uniform(rng, 1, 64)]), experts=experts,
+                top_k=rng.choice([1, 2, 2, 4]), cin=size(128, 4096), hidden=size(128, 8192), cout=size(128, 4096), dtype=dtype,
+                wtype=rng.choice([dtype, dtype, "i8"]), act=rng.choice(["gated", "gated", "relu"]), renormalize=rng.random() < 0.7)
+    if rng.random() < 0.6:
+        case["cout"] = case["cin"]
+    most = 8 * 3 * 4096 * 8192 // 2
+    while experts * _matrices(case) * case["hidden"] * max(case["cin"], case["cout"]) > most:
+        case["hidden"] = max(128, case["hidden"] // 2)
+        case["cin"], case["cout"] = (max(128, case["cin"] * 3 // 4), max(128, case["cout"] * 3 // 4)) if case["hidden"] == 128 else (case["cin"], case["cout"])
+    return case
+
+
+# --------------------------------------------------------------------------- #
+# inputs                                                                      #
+# --------------------------------------------------------------------------- #
+def _rows8(w):
+    """8-bit integers and a scale per row of w [..., K], as a program keeps its weights."""
+    scale = w.abs().amax(-1) / 127.0
+    return torch.round(w / scale[..., None]).to(torch.int8), scale
+
+
+def prepare(case, seed):
+    g = torch.Generator(device=DEVICE).manual_seed(int(seed))
+
+    def normal(*shape, std=1.0, dtype=torch.float32):
+        return torch.randn(*shape, generator=g, device=DEVICE, dtype=dtype).mul_(std)
+    dt = _TYPES[case["dtype"]]
+    if case["kind"] == "fc":
+        # activations behind a ReLU, rows of different brightness
+        x = normal(case["rows"], case["k"]).clamp_(min=0.0).mul_(torch.exp(normal(case["rows"], 1, std=0.5)))
+        wq, ws = _rows8(normal(case["cout"], case["k"], std=math.sqrt(2.0 / case["k"])))
+        return dict(case=case, x=x.to(dt), wq=wq, ws=ws, bias=normal(case["cout"], std=0.1))
+    E, cin, hid, cout = case["experts"], case["cin"], case["hidden"], case["cout"]
+    wdt = torch.bfloat16 if case["wtype"] == "i8" else dt
+    halves = 2 if case["act"] == "gated" else 1
+    s = dict(case=case, x=normal(case["tokens"], cin).to(dt), router=normal(E, cin, std=cin ** -0.5).to(dt), router_bias=normal(E, std=0.1),
+             up=normal(E, halves * hid, cin, std=cin ** -0.5, dtype=wdt), up_bias=normal(E, halves * hid, std=0.1),
+             down=normal(E, cout, hid, std=hid ** -0.5, dtype=wdt), down_bias=normal(E, cout, std=0.1), up_scale=None, down_scale=None)
+    if case["wtype"] == "i8":
+        for n in ("up", "down"):
+            both = [_rows8(w.float()) for w in s[n]]
+            s[n], s[n + "_scale"] = torch.stack([q for q, _ in both]), torch.stack([v for _, v in both])
+    return s
+
+
+# --------------------------------------------------------------------------- #
+# one pass                                                                    #
+# --------------------------------------------------------------------------- #
+def _fc_plain(s):
+    x = s["x"].float()
+    scale = x.abs().amax(1, keepdim=True) / 127.0
+    q = torch.round(x.double() / torch.where(scale > 0, scale, torch.ones_like(scale)).double()).float()      # (borders of a rounding)
+    out = torch.matmul(q, s["wq"].float().t()) * (scale * s["ws"]) + s["bias"]
+    if s["case"]["relu"]:
+        out = torch.where(out > 0, out, torch.zeros_like(out))
+    return out.to(s["x"].dtype).view(out.shape[0], 1, 1, -1)
+
+
+def _moe_plain(s):
+    c, x = s["case"], s["x"].float()
+    E, k, hid = c["experts"], c["top_k"], c["hidden"]
+    logits = torch.matmul(x, s["router"].float().t()) + s["router_bias"]
+    p = torch.exp(logits - logits.amax(1, keepdim=True))
+    p = p / p.sum(1, keepdim=True)
+    lower = torch.arange(E, device=x.device)[:, None] > torch.arange(E, device=x.device)      # [e][j]: j stands before e
+    rank = ((logits[:, None, :] > logits[:, :, None]) | ((logits[:, None, :] == logits[:, :, None]) & lower)).sum(2)
+    experts = (rank[:, None, :] == torch.arange(k, device=x.device)[:, None]).long().argmax(2)
+    gates = p.gather(1, experts)
+    if c["renormalize"]:
+        gates = gates / gates.sum(1, keepdim=True)
+    up, down = s["up"].float(), s["down"].float()
+    if c["wtype"] == "i8":
+        up, down = up * s["up_scale"][..., None], down * s["down_scale"][..., None]
+    u = torch.matmul(x, up.transpose(1, 2)) + s["up_bias"][:, None]             # every expert for every row: [E][T][...]
+    if c["act"] == "gated":
+        h = u[..., :hid] / (1.0 + torch.exp(-u[..., :hid])) * u[..., hid:]
+    else:
+        h = torch.where(u > 0, u, torch.zeros_like(u))
+    y = torch.matmul(h, down.transpose(1, 2)) + s["down_bias"][:, None]
+    weight = torch.zeros_like(p).scatter(1, experts, gates)                     # zero where an expert is not chosen
+    return dict(out=(y * weight.t()[..., None]).sum(0).to(s["x"].dtype), experts=experts.int(), gates=gates)
+
+
+def run(s):
+    c = s["case"]
+    if not own:
+        return _fc_plain(s) if c["kind"] == "fc" else _moe_plain(s)
+    from paper_1712_01670_amd import binding
+    if c["kind"] == "fc":
+        return binding.dc_fc_i8_layer(s["x"], s["wq"], s["ws"], s["bias"], c["relu"])
+    moe = dict(experts=c["experts"], top_k=c["top_k"], cin=c["cin"], hidden=c["hidden"], cout=c["cout"],
+               act=binding.DC_MOE_GATED if c["act"] == "gated" else binding.DC_MOE_RELU, renormalize=c["renormalize"])
+    out, experts, gates = binding.dc_moe_layer(moe, s["x"], s["router"], s["up"], s["down"], router_bias=s["router_bias"],
+                                               up_bias=s["up_bias"], down_bias=s["down_bias"], up_scale=s["up_scale"],
+                                               down_scale=s["down_scale"])
+    return dict(out=out, experts=experts, gates=gates)
+
+
+def work(case):
+    es = 2 if case["dtype"] == "bf16" else 4
+    if case["kind"] == "fc":
+        r, k, o = case["rows"], case["k"], case["cout"]
+        return dict(bytes=r * k * es + o * k + 8 * o + r * o * es, flops=2.0 * r * k * o)
+    T, E, k = case["tokens"], case["experts"], case["top_k"]
+    wes = 1 if case["wtype"] == "i8" else es
+    halves = _matrices(case) - 1
+    one = case["hidden"] * (halves * case["cin"] + case["cout"])                # weights of an expert
+    rows = halves * case["hidden"] + case["cout"]                               # its channels
+    read = E * (1.0 - (1.0 - k / E) ** T)                                       # experts that some row chose, on average
+    return dict(bytes=read * (one * wes + rows * (8 if wes == 1 else 4)) + E * (case["cin"] * es + 4) +
+                T * ((case["cin"] + case["cout"]) * es + 8 * k),
+                flops=2.0 * T * (k * one + E * case["cin"]))
+
+
+# --------------------------------------------------------------------------- #
+# the same from the definition, in 64 bits                                    #
+# --------------------------------------------------------------------------- #
+def _fc_exact(s):
+    out = []
+    wt = s["wq"].double().t().contiguous() * s["ws"].double()
+    for x in s["x"].double().split(4096):
+        scale = (x.abs().max(dim=1).values / 127.0).float().double()[:, None]   # (a scale is a number of 32 bits)
+        q = torch.where(scale > 0, x / scale, torch.zeros_like(x)).round()
+        y = (q @ wt) * scale + s["bias"].double()
+        out.append(y.clamp(min=0.0) if s["case"]["relu"] else y)
+    return torch.cat(out)[:, None, None, :]
+
+
+def _moe_exact(s):
+    c, x = s["case"], s["x"].double()
+    p = torch.softmax(x @ s["router"].double().t() + s["router_bias"].double(), dim=1)
+    order = torch.sort(p, dim=1, descending=True, stable=True).indices[:, :c["top_k"]]
+    gates = torch.gather(p, 1, order)
+    if c["renormalize"]:
+        gates = gates / gates.sum(1, keepdim=True)
+    out = torch.zeros(c["tokens"], c["cout"], dtype=torch.float64, device=x.device)
+    for e in range(c["experts"]):
+        rows, slot = (order == e).nonzero(as_tuple=True)
+        if rows.numel() == 0:
+            continue
+        w1, w2 = s["up"][e].double(), s["down"][e].double()
+        if c["wtype"] == "i8":
+            w1, w2 = w1 * s["up_scale"][e].double()[:, None], w2 * s["down_scale"][e].double()[:, None]
+        u = x[rows] @ w1.t() + s["up_bias"][e].double()
+        h = torch.nn.functional.silu(u[:, :c["hidden"]]) * u[:, c["hidden"]:] if c["act"] == "gated" else u.relu()
+        out.index_add_(0, rows, (h @ w2.t() + s["down_bias"][e].double()) * gates[rows, slot][:, None])
+    return dict(out=out, experts=order.int(), gates=gates)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    return _fc_exact(s) if case["kind"] == "fc" else _moe_exact(s)
