@@ -2,7 +2,7 @@
 
 Both are what a program runs behind its feature maps, on one row per video stream, or (the product) on one row per pixel:
 
-* ``fc``   ``dc_fc_i8_layer``: rows in fp32 or bf16 are rounded to 8-bit integers with a scale of their own, multiplied with
+* ``fc``   ``dc_fc_quant_layer``: rows in fp32 or bf16 are rounded to 8-bit integers with a scale of their own, multiplied with
            8-bit weights (a scale per output channel) and scaled back; bias and ReLU as in ``dc_fc_layer``.
 * ``moe``  ``dc_moe_layer``: a router picks ``top_k`` of ``experts`` pairs of fully-connected layers for every row and adds
            their outputs, weighted by the router's softmax.  Weights in the rows' type or in 8 bits with a scale per channel.
@@ -166,7 +166,7 @@ def run(s):
         return _fc_plain(s) if c["kind"] == "fc" else _moe_plain(s)
     from paper_1712_01670_amd import binding
     if c["kind"] == "fc":
-        return binding.dc_fc_i8_layer(s["x"], s["wq"], s["ws"], s["bias"], c["relu"])
+        return binding.dc_fc_quant_layer(s["x"], s["wq"], s["ws"], s["bias"], c["relu"])
     moe = dict(experts=c["experts"], top_k=c["top_k"], cin=c["cin"], hidden=c["hidden"], cout=c["cout"],
                act=binding.DC_MOE_GATED if c["act"] == "gated" else binding.DC_MOE_RELU, renormalize=c["renormalize"])
     out, experts, gates = binding.dc_moe_layer(moe, s["x"], s["router"], s["up"], s["down"], router_bias=s["router_bias"],
