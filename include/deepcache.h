@@ -486,6 +486,34 @@ int32_t dc_fc_layer(const void* in, const void* weights, const float* bias, void
                     int32_t cout, int32_t relu, int32_t dtype, void* stream);
 int32_t dc_softmax_layer(const void* in, void* out, size_t n_pixels, int32_t C, int32_t dtype, void* stream);
 
+/*
+ * Rows in 8-bit integers with a scale each: scales[r] = max_k |in[r][k]| / 127 in fp32, q[r][k] = in[r][k] / scales[r] rounded
+ * half to even (the exact quotient), so that q[r][k] scales[r] stands for in[r][k].  This is how weights get into the form
+ * that dc_fc_quant_layer takes (once: a row is an output channel).  A row of zeros has the scale 0; a row that holds a NaN or
+ * an infinity has the scale NaN and zeros, so that every product with it is NaN.  Scales among the subnormal
+ * numbers (rows below 1e-36) are coarse; q then saturates at +-127.
+ *   in      dev [n_rows][K] in `dtype`;  q  dev int8 [n_rows][K];  scales  dev fp32 [n_rows].  No alignment is asked for
+ *           beyond the types' own.  1 <= K <= 131072.
+ */
+int32_t dc_quantize_rows(const void* in, size_t n_rows, size_t K, int32_t dtype, int8_t* q, float* scales, void* stream);
+
+/*
+ * Fully-connected layer in 8-bit integers: dc_fc_layer whose weights are 8-bit integers with a scale per output channel and
+ * whose input rows are rounded to 8 bits with a scale per row (as by dc_quantize_rows) within the call:
+ *   out[r][o] = act(bias[o] + row_scale[r] weight_scales[o] sum_k q[r][k] weights[o][k])
+ * The integer sum is exact, so a row's result depends neither on the other rows nor on their number.  Rows are streams
+ * ([n_streams][K], the whole map of a stream) or, for a 1x1 layer, pixels ([n_streams * H * W][cin]).
+ *   in        dev [n_rows][K] in `dtype`, out dev [n_rows][cout] in `dtype` (must not overlap `in`)
+ *   weights   dev int8 [cout][K], weight_scales dev fp32 [cout], bias dev fp32 [cout] or NULL
+ *   ws_dev    dev workspace of at least dc_fc_quant_workspace_bytes, 256-byte aligned; calls that may overlap in time need
+ *             workspaces of their own
+ * 1 <= K <= 131072 (the sum fits 32 bits).  relu: 0 or 1; a NaN stays one.  Rows with a NaN or an infinity give NaN rows.
+ */
+int32_t dc_fc_quant_workspace_bytes(int32_t n_rows, size_t K, int32_t cout, size_t* bytes);
+int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* weight_scales, const float* bias, void* out,
+                       int32_t n_rows, size_t K, int32_t cout, int32_t relu, int32_t dtype,
+                       void* ws_dev, size_t ws_dev_bytes, void* stream);
+
 /* Workspace sizes for dc_run_stack. */
 int32_t dc_stack_workspace_bytes(const dc_layer* layers, int32_t n_layers, int32_t n_streams,
                                  int32_t H, int32_t W, int32_t C, int32_t block,

@@ -27,7 +27,8 @@ EXPORTS = ["dc_status_string", "dc_profile_create", "dc_profile_destroy", "dc_pr
            "dc_profile_elapsed_ms", "dc_overlap_create", "dc_overlap_destroy", "dc_overlap_pipeline", "dc_overlap_replay", "dc_overlap_stats", "dc_prefetch_match", "dc_conv_tuning", "dc_conv_kernel_name", "dc_conv_tile_shape", "dc_match_blocks", "dc_match_blocks_ds", "dc_match_blocks_opt", "dc_propagate_regions", "dc_propagate_regions_opt", "dc_conv_workspace_bytes",
            "dc_packed_weights_bytes", "dc_pack_conv_weights", "dc_cached_conv_layer", "dc_frame_to_tensor", "dc_torus_read", "dc_maxpool_layer", "dc_add_layer", "dc_avgpool_layer", "dc_lrn_layer", "dc_concat_layer", "dc_fc_layer", "dc_softmax_layer",
            "dc_stack_workspace_bytes", "dc_run_stack", "dc_stack_stats_fetch", "dc_cached_conv_layer_noalloc",
-           "dc_propagate_masks_size", "dc_propagate_masks", "dc_probe_mfma_rate"]
+           "dc_propagate_masks_size", "dc_propagate_masks", "dc_probe_mfma_rate",
+           "dc_quantize_rows", "dc_fc_quant_workspace_bytes", "dc_fc_quant_layer"]
 
 
 class DcError(RuntimeError):
@@ -118,6 +119,9 @@ def lib():
         L.dc_concat_layer.argtypes = [vp, vp, i32, vp, sz, i32, vp]
         L.dc_fc_layer.argtypes = [vp, vp, vp, vp, i32, sz, i32, i32, i32, vp]
         L.dc_softmax_layer.argtypes = [vp, vp, sz, i32, i32, vp]
+        L.dc_quantize_rows.argtypes = [vp, sz, sz, i32, vp, vp, vp]
+        L.dc_fc_quant_workspace_bytes.argtypes = [i32, sz, i32, C.POINTER(sz)]
+        L.dc_fc_quant_layer.argtypes = [vp, vp, vp, vp, vp, i32, sz, i32, i32, i32, vp, sz, vp]
         L.dc_stack_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
         L.dc_run_stack.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, u32, vp, i32, vp,
                                    vp, vp, vp, vp, vp, i32, vp, vp, sz, vp, sz, vp, vp, vp]
@@ -151,6 +155,44 @@ def layers_to_c(layers):
     for i, L in enumerate(layers):
         arr[i] = Layer(*[(float if ct is C.c_float else int)(L[f] if f in L else synth.LAYER_DEFAULTS[f]) for f, ct in Layer._fields_])
     return arr
+
+
+class _Here:
+    def __enter__(self):
+        pass
+
+    def __exit__(self, *exc):
+        pass
+
+
+_HERE_DEVICE = _Here()
+
+
+def _on(device):
+    """Makes `device` the current one (whose current stream takes the call) unless it is."""
+    return _HERE_DEVICE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+
+
+def _rows_dtype(fn, x):
+    """DC_F32 or DC_BF16 of a contiguous cuda tensor of rows; anything else is an error."""
+    if not x.is_cuda or not x.is_contiguous() or x.dim() < 1:
+        raise ValueError(f"{fn}: the rows have to be a contiguous cuda tensor")
+    if x.dtype == torch.bfloat16:
+        return DC_BF16
+    if x.dtype != torch.float32:
+        raise ValueError(f"{fn}: {x.dtype} rows (float32 or bfloat16)")
+    return DC_F32
+
+
+def _want(fn, t, dtype, shape, device):
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{fn}: wants a contiguous {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
+                         + ("" if t.is_contiguous() else ", not contiguous"))
+
+
+def _scratch(n_bytes, device):
+    """Workspace of one call, from torch's allocator: ordered by the current stream like any tensor, also under capture."""
+    return torch.empty(n_bytes, dtype=torch.uint8, device=device) if n_bytes else None
 
 
 def torch_dtype(dtype):
@@ -483,6 +525,39 @@ def dc_fc_layer(x, w, bias, relu):
     out = torch.empty((n, 1, 1, cout), dtype=x.dtype, device=x.device)
     _check("dc_fc_layer", lib().dc_fc_layer(_ptr(x), _ptr(w), _ptr(bias) if bias is not None else None, _ptr(out), n,
                                             C.c_size_t(K), cout, int(relu), dtype, _stream()))
+    return out
+
+
+def dc_quantize_rows(x):
+    """8-bit form of the rows of x [..., K] (cuda, fp32 or bf16): (int8 tensor of x's shape, fp32 scales of its leading shape).
+    A matrix of weights [cout][K] becomes the weights of dc_fc_quant_layer."""
+    dtype = _rows_dtype("dc_quantize_rows", x)
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    with _on(x.device):
+        _check("dc_quantize_rows", lib().dc_quantize_rows(x.data_ptr(), scales.numel(), x.shape[-1], dtype, q.data_ptr(),
+                                                          scales.data_ptr(), _stream()))
+    return q, scales
+
+
+def dc_fc_quant_layer(x, weights, scales, bias, relu):
+    """dc_fc_layer in 8-bit integers.  x [n][...] (cuda, fp32 or bf16), a row being everything behind the first axis; weights
+    int8 [cout][K] and scales fp32 [cout] as by dc_quantize_rows, bias fp32 [cout] or None.  Returns [n][1][1][cout]."""
+    dtype = _rows_dtype("dc_fc_quant_layer", x)
+    n, cout = x.shape[0], weights.shape[0]
+    K = x.numel() // n if n else 0
+    _want("dc_fc_quant_layer", weights, torch.int8, (cout, K), x.device)
+    _want("dc_fc_quant_layer", scales, torch.float32, (cout,), x.device)
+    if bias is not None:
+        _want("dc_fc_quant_layer", bias, torch.float32, (cout,), x.device)
+    out = torch.empty((n, 1, 1, cout), dtype=x.dtype, device=x.device)
+    with _on(x.device):
+        need = C.c_size_t()
+        _check("dc_fc_quant_workspace_bytes", lib().dc_fc_quant_workspace_bytes(n, K, cout, C.byref(need)))
+        ws = _scratch(need.value, x.device)
+        _check("dc_fc_quant_layer", lib().dc_fc_quant_layer(
+            x.data_ptr(), weights.data_ptr(), scales.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), n, K, cout,
+            int(relu), dtype, None if ws is None else ws.data_ptr(), need.value, _stream()))
     return out
 
 

@@ -667,6 +667,39 @@ int32_t dc_fc_layer(const void* in, const void* weights, const float* bias, void
     return DC_OK;
 }
 
+int32_t dc_quantize_rows(const void* in, size_t n_rows, size_t K, int32_t dtype, int8_t* q, float* scales, void* stream) {
+    if (!in || !q || !scales) return DC_ERR_NULL_PTR;
+    if (dtype != DC_F32 && dtype != DC_BF16) return DC_ERR_INVALID_ARG;
+    if (n_rows < 1 || K < 1) return DC_ERR_INVALID_ARG;
+    if (K > kI8MaxK || n_rows > 0x7fffffffull) return DC_ERR_UNSUPPORTED;
+    DC_TRY_HIP(launch_quantize_rows(in, dtype, n_rows, (int)K, q, scales, as_stream(stream)));
+    return DC_OK;
+}
+
+int32_t dc_fc_quant_workspace_bytes(int32_t n_rows, size_t K, int32_t cout, size_t* bytes) {
+    if (!bytes) return DC_ERR_NULL_PTR;
+    if (n_rows < 1 || K < 1 || cout < 1) return DC_ERR_INVALID_ARG;
+    if (K > kI8MaxK) return DC_ERR_UNSUPPORTED;
+    *bytes = fc_i8_workspace(n_rows, (int)K);
+    return DC_OK;
+}
+
+int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* weight_scales, const float* bias, void* out,
+                       int32_t n_rows, size_t K, int32_t cout, int32_t relu, int32_t dtype, void* ws_dev, size_t ws_dev_bytes,
+                       void* stream) {
+    if (!in || !weights || !weight_scales || !out) return DC_ERR_NULL_PTR;
+    if (dtype != DC_F32 && dtype != DC_BF16) return DC_ERR_INVALID_ARG;
+    if (relu != 0 && relu != 1) return DC_ERR_INVALID_ARG;
+    size_t need = 0;
+    const int rc = dc_fc_quant_workspace_bytes(n_rows, K, cout, &need);
+    if (rc) return rc;
+    if (need && !ws_dev) return DC_ERR_NULL_PTR;
+    if (ws_dev_bytes < need) return DC_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws_dev) % 256 || in == out) return DC_ERR_INVALID_ARG;
+    DC_TRY_HIP(launch_fc_i8(in, weights, weight_scales, bias, out, n_rows, (int)K, cout, relu, dtype, ws_dev, as_stream(stream)));
+    return DC_OK;
+}
+
 int32_t dc_softmax_layer(const void* in, void* out, size_t n_pixels, int32_t C, int32_t dtype, void* stream) {
     if (!in || !out) return DC_ERR_NULL_PTR;
     if (dtype != DC_F32 && dtype != DC_BF16) return DC_ERR_INVALID_ARG;

@@ -192,6 +192,13 @@ hipError_t launch_softmax(const void* in, void* out, size_t n_pixels, int C, int
 // x: [n_streams][K], w: [cout][K], out: [n_streams][cout]
 hipError_t launch_fc(const void* x, const void* w, const float* bias, void* out, int n_streams, size_t K, int cout,
                      int relu, int dtype, hipStream_t st);
+// ---- fully-connected layers in 8-bit integers (dc_fc_quant.hip) ----
+constexpr size_t kI8MaxK = 131072;       // 127 * 127 * K < 2^31
+// q [n_rows][K], scales [n_rows]
+hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, int8_t* q, float* scales, hipStream_t st);
+size_t fc_i8_workspace(int n_rows, int K);
+hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
+                        int dtype, void* ws, hipStream_t st);
 // Producer tensors of a DC_CONCAT layer in channel order; returns their number (2..4).
 int concat_inputs(const dc_layer& l, int* ids);
 
