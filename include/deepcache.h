@@ -51,6 +51,7 @@ enum {
 };
 
 enum { DC_F32 = 0, DC_BF16 = 1 };
+enum { DC_I8 = 2 };            /* weights only (dc_moe): 8-bit integers with a scale per row, as by dc_quantize_rows */
 /* Layer types: the rows of Table 2.  Only DC_CONV is cached (Section 5); the others are computed in full. */
 enum { DC_CONV = 0, DC_MAXPOOL = 1, DC_RELU = 2, DC_ADD = 3, DC_LRN = 4, DC_CONCAT = 5, DC_FC = 6, DC_SOFTMAX = 7,
        DC_AVGPOOL = 8 };
@@ -513,6 +514,48 @@ int32_t dc_fc_quant_workspace_bytes(int32_t n_rows, size_t K, int32_t cout, size
 int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* weight_scales, const float* bias, void* out,
                        int32_t n_rows, size_t K, int32_t cout, int32_t relu, int32_t dtype,
                        void* ws_dev, size_t ws_dev_bytes, void* stream);
+
+/*
+ * Mixture-of-experts layer for a few tokens (a row of features per stream): a router chooses top_k of `experts` pairs of
+ * fully-connected layers for every token,
+ *   l = router x + router_bias;  p = softmax(l) over all experts;  the top_k experts with the largest l are chosen (equal: the
+ *   lowest index first);  gate_e = p_e, with `renormalize` p_e / (sum of the chosen p)
+ *   h_e = relu(up_e x + up_bias_e)                                         act = DC_MOE_RELU
+ *   h_e = silu(u) * v with u, v the halves of up_e x + up_bias_e           act = DC_MOE_GATED, silu(u) = u / (1 + exp(-u))
+ *   out = sum over the chosen e of gate_e (down_e h_e + down_bias_e)
+ * All sums are held in fp32 (h_e too: in bf16 as two numbers each) and the output is rounded once.  An expert whose logit is
+ * -inf (a router_bias of -inf switches an expert off) is never chosen; a token left with fewer than top_k experts has the
+ * expert -1 and the gate 0 in the last places, one left with none an output of zeros.  A NaN among a token's logits makes its
+ * gates and its output NaN and leaves the other tokens alone.
+ *   in       dev [n_tokens][cin] in `dtype`, out dev [n_tokens][cout] in `dtype` (must not overlap `in`)
+ *   router   dev [experts][cin] in `dtype`, router_bias dev fp32 [experts] or NULL
+ *   up       dev [experts][hidden][cin], gated: [experts][2][hidden][cin]; down dev [experts][cout][hidden]; both in `wtype`,
+ *            which is `dtype` or DC_I8; DC_I8 takes fp32 scales per row: up_scale [experts][(2)][hidden], down_scale [experts][cout]
+ *   up_bias, down_bias   dev fp32, of the scales' shapes, or NULL
+ *   experts_out, gates_out   optional dev int32 / fp32 [n_tokens][top_k]: the choice, in falling order of the logits
+ *   ws_dev   dev workspace of at least dc_moe_workspace_bytes, 256-byte aligned; calls that may overlap in time need
+ *            workspaces of their own
+ * The expert's weights are read once for up to 64 tokens.  Limits (DC_ERR_UNSUPPORTED): 256 experts, top_k 16, 512 tokens;
+ * top_k <= experts.  Rows need no alignment beyond their types' own.
+ */
+enum { DC_MOE_RELU = 0, DC_MOE_GATED = 1 };
+typedef struct {
+    int32_t experts, top_k, cin, hidden, cout;
+    int32_t act;              /* DC_MOE_RELU or DC_MOE_GATED */
+    int32_t renormalize;      /* 0 or 1 */
+    int32_t wtype;            /* storage of up and down: the call's dtype, or DC_I8 */
+} dc_moe;
+typedef struct {
+    const void* router;
+    const float* router_bias;
+    const void* up;
+    const float *up_scale, *up_bias;
+    const void* down;
+    const float *down_scale, *down_bias;
+} dc_moe_weights;
+int32_t dc_moe_workspace_bytes(const dc_moe* moe, int32_t n_tokens, size_t* bytes);
+int32_t dc_moe_layer(const dc_moe* moe, const dc_moe_weights* weights, const void* in, void* out, int32_t* experts_out,
+                     float* gates_out, int32_t n_tokens, int32_t dtype, void* ws_dev, size_t ws_dev_bytes, void* stream);
 
 /* Workspace sizes for dc_run_stack. */
 int32_t dc_stack_workspace_bytes(const dc_layer* layers, int32_t n_layers, int32_t n_streams,

@@ -20,6 +20,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libdeepcache.so")
 
 DC_F32, DC_BF16 = 0, 1
+DC_I8 = 2                      # weights of dc_moe_layer
+DC_MOE_RELU, DC_MOE_GATED = 0, 1
 STATUS = {0: "DC_OK", -1: "DC_ERR_INVALID_ARG", -2: "DC_ERR_NULL_PTR", -3: "DC_ERR_BAD_SHAPE",
           -4: "DC_ERR_UNSUPPORTED", -5: "DC_ERR_WORKSPACE", -6: "DC_ERR_CAPACITY", -7: "DC_ERR_HIP"}
 
@@ -28,7 +30,8 @@ EXPORTS = ["dc_status_string", "dc_profile_create", "dc_profile_destroy", "dc_pr
            "dc_packed_weights_bytes", "dc_pack_conv_weights", "dc_cached_conv_layer", "dc_frame_to_tensor", "dc_torus_read", "dc_maxpool_layer", "dc_add_layer", "dc_avgpool_layer", "dc_lrn_layer", "dc_concat_layer", "dc_fc_layer", "dc_softmax_layer",
            "dc_stack_workspace_bytes", "dc_run_stack", "dc_stack_stats_fetch", "dc_cached_conv_layer_noalloc",
            "dc_propagate_masks_size", "dc_propagate_masks", "dc_probe_mfma_rate",
-           "dc_quantize_rows", "dc_fc_quant_workspace_bytes", "dc_fc_quant_layer"]
+           "dc_quantize_rows", "dc_fc_quant_workspace_bytes", "dc_fc_quant_layer",
+           "dc_moe_workspace_bytes", "dc_moe_layer"]
 
 
 class DcError(RuntimeError):
@@ -73,6 +76,14 @@ class StackStats(C.Structure):
 class OverlapCounters(C.Structure):
     _fields_ = [(n, C.c_int64) for n in ("frames", "replayed", "recorded", "dropped", "evicted", "failed", "recuts")] + \
                [("stages", C.c_int32), ("last_layers", C.c_int32)]
+
+
+class Moe(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("experts", "top_k", "cin", "hidden", "cout", "act", "renormalize", "wtype")]
+
+
+class MoeWeights(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("router", "router_bias", "up", "up_scale", "up_bias", "down", "down_scale", "down_bias")]
 
 
 _lib = None
@@ -122,6 +133,8 @@ def lib():
         L.dc_quantize_rows.argtypes = [vp, sz, sz, i32, vp, vp, vp]
         L.dc_fc_quant_workspace_bytes.argtypes = [i32, sz, i32, C.POINTER(sz)]
         L.dc_fc_quant_layer.argtypes = [vp, vp, vp, vp, vp, i32, sz, i32, i32, i32, vp, sz, vp]
+        L.dc_moe_workspace_bytes.argtypes = [C.POINTER(Moe), i32, C.POINTER(sz)]
+        L.dc_moe_layer.argtypes = [C.POINTER(Moe), C.POINTER(MoeWeights), vp, vp, vp, vp, i32, i32, vp, sz, vp]
         L.dc_stack_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
         L.dc_run_stack.argtypes = [vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, i32, u32, vp, i32, vp,
                                    vp, vp, vp, vp, vp, i32, vp, vp, sz, vp, sz, vp, vp, vp]
@@ -559,6 +572,39 @@ def dc_fc_quant_layer(x, weights, scales, bias, relu):
             x.data_ptr(), weights.data_ptr(), scales.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), n, K, cout,
             int(relu), dtype, None if ws is None else ws.data_ptr(), need.value, _stream()))
     return out
+
+
+def dc_moe_layer(moe, x, router, up, down, router_bias=None, up_bias=None, down_bias=None, up_scale=None, down_scale=None):
+    """Mixture-of-experts layer over the rows of x [n][cin] (cuda, fp32 or bf16).  moe: dict(experts, top_k, cin, hidden, cout,
+    act=DC_MOE_RELU | DC_MOE_GATED, renormalize); router [experts][cin] in x's type; up [experts][hidden][cin] (gated:
+    [experts][2 * hidden][cin], the gates' rows first) and down [experts][cout][hidden] in x's type, or int8 with scales per row
+    (dc_quantize_rows); biases fp32 or None.  Returns (out [n][cout], experts int32 [n][top_k], gates fp32 [n][top_k])."""
+    fn = "dc_moe_layer"
+    dtype = _rows_dtype(fn, x)
+    E, k, cin, hidden, cout = (int(moe[f]) for f in ("experts", "top_k", "cin", "hidden", "cout"))
+    act = int(moe["act"])
+    rows = hidden * (2 if act == DC_MOE_GATED else 1)
+    int8 = up.dtype == torch.int8
+    dev, n = x.device, x.shape[0]
+    _want(fn, x, x.dtype, (n, cin), dev)
+    _want(fn, router, x.dtype, (E, cin), dev)
+    _want(fn, up, torch.int8 if int8 else x.dtype, (E, rows, cin), dev)
+    _want(fn, down, up.dtype, (E, cout, hidden), dev)
+    for t, shape in ((router_bias, (E,)), (up_bias, (E, rows)), (down_bias, (E, cout)), (up_scale, (E, rows)), (down_scale, (E, cout))):
+        if t is not None:
+            _want(fn, t, torch.float32, shape, dev)
+    m = Moe(E, k, cin, hidden, cout, act, int(moe["renormalize"]), DC_I8 if int8 else dtype)
+    p = [t.data_ptr() if t is not None else None for t in (router, router_bias, up, up_scale, up_bias, down, down_scale, down_bias)]
+    out = torch.empty((n, cout), dtype=x.dtype, device=dev)
+    experts = torch.empty((n, k), dtype=torch.int32, device=dev)
+    gates = torch.empty((n, k), dtype=torch.float32, device=dev)
+    with _on(dev):
+        need = C.c_size_t()
+        _check("dc_moe_workspace_bytes", lib().dc_moe_workspace_bytes(C.byref(m), n, C.byref(need)))
+        ws = _scratch(need.value, dev)
+        _check(fn, lib().dc_moe_layer(C.byref(m), C.byref(MoeWeights(*p)), x.data_ptr(), out.data_ptr(), experts.data_ptr(), gates.data_ptr(),
+                                      n, dtype, ws.data_ptr(), need.value, _stream()))
+    return out, experts, gates
 
 
 def dc_softmax_layer(x):

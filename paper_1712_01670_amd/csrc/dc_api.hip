@@ -700,6 +700,35 @@ int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* we
     return DC_OK;
 }
 
+int32_t dc_moe_workspace_bytes(const dc_moe* moe, int32_t n_tokens, size_t* bytes) {
+    if (!moe || !bytes) return DC_ERR_NULL_PTR;
+    const dc_moe& m = *moe;
+    if (n_tokens < 1 || m.experts < 1 || m.top_k < 1 || m.cin < 1 || m.hidden < 1 || m.cout < 1 || m.top_k > m.experts) return DC_ERR_INVALID_ARG;
+    if (m.act != DC_MOE_RELU && m.act != DC_MOE_GATED) return DC_ERR_INVALID_ARG;
+    if (m.renormalize != 0 && m.renormalize != 1) return DC_ERR_INVALID_ARG;
+    if (m.wtype != DC_F32 && m.wtype != DC_BF16 && m.wtype != DC_I8) return DC_ERR_INVALID_ARG;
+    if (m.experts > kMoeMaxExperts || m.top_k > kMoeMaxTopK || n_tokens > kMoeMaxTokens) return DC_ERR_UNSUPPORTED;
+    if (m.cin > (1 << 24) || m.hidden > (1 << 24) || m.cout > (1 << 24)) return DC_ERR_UNSUPPORTED;
+    *bytes = moe_workspace(m, n_tokens);
+    return DC_OK;
+}
+
+int32_t dc_moe_layer(const dc_moe* moe, const dc_moe_weights* weights, const void* in, void* out, int32_t* experts_out,
+                     float* gates_out, int32_t n_tokens, int32_t dtype, void* ws_dev, size_t ws_dev_bytes, void* stream) {
+    if (!moe || !weights || !in || !out || !weights->router || !weights->up || !weights->down) return DC_ERR_NULL_PTR;
+    if (dtype != DC_F32 && dtype != DC_BF16) return DC_ERR_INVALID_ARG;
+    size_t need = 0;
+    const int rc = dc_moe_workspace_bytes(moe, n_tokens, &need);
+    if (rc) return rc;
+    if (moe->wtype != DC_I8 && moe->wtype != dtype) return DC_ERR_INVALID_ARG;
+    if (moe->wtype == DC_I8 && (!weights->up_scale || !weights->down_scale)) return DC_ERR_NULL_PTR;
+    if (!ws_dev) return DC_ERR_NULL_PTR;
+    if (ws_dev_bytes < need) return DC_ERR_WORKSPACE;
+    if (reinterpret_cast<uintptr_t>(ws_dev) % 256 || in == out) return DC_ERR_INVALID_ARG;
+    DC_TRY_HIP(launch_moe(*moe, *weights, in, out, experts_out, gates_out, n_tokens, dtype, ws_dev, as_stream(stream)));
+    return DC_OK;
+}
+
 int32_t dc_softmax_layer(const void* in, void* out, size_t n_pixels, int32_t C, int32_t dtype, void* stream) {
     if (!in || !out) return DC_ERR_NULL_PTR;
     if (dtype != DC_F32 && dtype != DC_BF16) return DC_ERR_INVALID_ARG;

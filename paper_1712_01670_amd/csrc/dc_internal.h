@@ -199,6 +199,11 @@ hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, 
 size_t fc_i8_workspace(int n_rows, int K);
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
                         int dtype, void* ws, hipStream_t st);
+// ---- mixture-of-experts layer (dc_moe.hip) ----
+constexpr int kMoeMaxExperts = 256, kMoeMaxTopK = 16, kMoeMaxTokens = 512;
+size_t moe_workspace(const dc_moe& m, int n_tokens);
+hipError_t launch_moe(const dc_moe& m, const dc_moe_weights& w, const void* in, void* out, int32_t* experts, float* gates, int n_tokens, int dtype,
+                      void* ws, hipStream_t st);
 // Producer tensors of a DC_CONCAT layer in channel order; returns their number (2..4).
 int concat_inputs(const dc_layer& l, int* ids);
 
