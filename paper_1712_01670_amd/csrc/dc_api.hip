@@ -680,7 +680,7 @@ int32_t dc_fc_quant_workspace_bytes(int32_t n_rows, size_t K, int32_t cout, size
     if (!bytes) return DC_ERR_NULL_PTR;
     if (n_rows < 1 || K < 1 || cout < 1) return DC_ERR_INVALID_ARG;
     if (K > kI8MaxK) return DC_ERR_UNSUPPORTED;
-    *bytes = fc_i8_workspace(n_rows, (int)K);
+    *bytes = fc_i8_workspace(n_rows, (int)K, cout);
     return DC_OK;
 }
 

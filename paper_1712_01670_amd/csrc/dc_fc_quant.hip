@@ -6,6 +6,7 @@
 #include <hip/hip_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "dc_internal.h"
 
@@ -171,6 +172,12 @@ __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __hip_bfloat16 to_out<__hip_bfloat16>(float v) { return __float2bfloat16(v); }
 
+// A sum's way out, the same operations in every kernel.
+__device__ __forceinline__ float finish(int sum, float sw, float sx, float bias, int relu) {
+    const float v = fmaf((float)sum * sw, sx, bias);
+    return relu && v < 0.f ? 0.f : v;
+}
+
 // 16 weights of a row from k0 on; past the row's end zeros.
 __device__ __forceinline__ intx4 weights16(const int8_t* __restrict__ row, int k0, int K) {
     if (k0 + 16 <= K) return *reinterpret_cast<const intx4_any*>(row + k0);
@@ -182,6 +189,7 @@ __device__ __forceinline__ intx4 weights16(const int8_t* __restrict__ row, int k
 // A workgroup takes 16 channels x NB * 16 rows; its wavefronts deal the tiles of K among themselves and add their integer
 // sums through LDS.
 constexpr int kI8Waves = 8;
+constexpr int kI8FewRows = 64;
 template <typename T, int NB>
 __global__ __launch_bounds__(kI8Waves * 64) void fc_i8_rows_kernel(FcI8 P) {
     __shared__ intx4 red[kI8Waves][NB][64];
@@ -218,22 +226,178 @@ __global__ __launch_bounds__(kI8Waves * 64) void fc_i8_rows_kernel(FcI8 P) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (o + e >= P.cout) break;
-            float v = (float)sum[e] * P.sw[o + e] * sx;
-            if (P.bias) v += P.bias[o + e];
-            if (P.relu) v = v > 0.f || v != v ? v : 0.f;
-            out[o + e] = to_out<T>(v);
+            out[o + e] = to_out<T>(finish(sum[e], P.sw[o + e], sx, P.bias ? P.bias[o + e] : 0.f, P.relu));
         }
     }
 }
 
+// Many rows: a GEMM of MT * 16 rows x NT * 16 channels per workgroup.  Both operands come through LDS in stages of 64 bytes of K
+// by direct loads, STAGES - 1 of them on their way while one is multiplied; a barrier a stage.  A wavefront's part is
+// MT / WM row tiles x NT / WN channel tiles, which is what a fragment read from LDS serves.
+// The rows are tiles as they are (fragments of 1 KiB: no bank is asked twice).  Weights come from [cout][K] when their rows are
+// whole aligned vectors (an instruction brings 16 rows of 64 bytes, four lanes a row; the four vectors of row r are stored in the
+// order v ^ (r / 2 % 4), so that eight neighbouring fragment lanes ask 128 different bytes), otherwise from a copy in
+// tiles (W_TILED).  What lies behind the end of a row of weights meets zeros of the input row; what lies behind an operand's
+// end reads as zero.
+constexpr int kBufferFlags = 0x00020000;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool W_TILED>
+__global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
+    constexpr int WAVES = WM * WN, XI = MT / WAVES, WI = NT / WAVES, UM = MT / WM, UN = NT / WN;
+    static_assert(MT % WAVES == 0 && NT % WAVES == 0, "every wavefront loads as many tiles of either operand");
+    constexpr int kStage = (MT + NT) * 1024;
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
+    // workgroup -> tile: every XCD (workgroup number modulo 8) takes a run of the tiles, which go down columns of 8 row tiles
+    const int n_m = (P.n_rows + MT * 16 - 1) / (MT * 16), n_n = (P.cout + NT * 16 - 1) / (NT * 16);
+    int tm, tn;
+    {
+        const int n = n_m * n_n, xcd = blockIdx.x & 7, j = blockIdx.x >> 3, per = n >> 3, more = n & 7;
+        const int at = xcd * per + min(xcd, more) + j;
+        const int band = at / (8 * n_n), left = min(8, n_m - band * 8), in = at - band * 8 * n_n;
+        tm = band * 8 + in % left;
+        tn = in / left;
+    }
+    const int m0 = tm * MT, o0 = tn * (NT * 16);           // first row tile, first channel
+    const int m_tiles = min(MT, (P.n_rows + 15) / 16 - m0), chans = min(NT * 16, P.cout - o0);
+    const size_t tile_row = (size_t)P.n_tiles * 1024;
+    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t*>(P.xq) + m0 * tile_row, 0, (uint32_t)(m_tiles * tile_row), kBufferFlags);
+    const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(
+        const_cast<int8_t*>(P.w) + (W_TILED ? (o0 >> 4) * tile_row : (size_t)o0 * P.K), 0,
+        (uint32_t)(W_TILED ? (chans + 15) / 16 * tile_row : (size_t)chans * P.K), kBufferFlags);
+    uint32_t xo[XI], wo[WI];
+#pragma unroll
+    for (int i = 0; i < XI; ++i) xo[i] = (uint32_t)((i * WAVES + wave) * tile_row) + lane * 16;
+#pragma unroll
+    for (int i = 0; i < WI; ++i) {
+        const int t = i * WAVES + wave, r = lane >> 2;
+        wo[i] = W_TILED ? (uint32_t)(t * tile_row) + lane * 16 : (uint32_t)(t * 16 + r) * P.K + (((lane & 3) ^ ((r / 2) & 3)) << 4);
+    }
+    auto issue = [&](int buf) {                            // the next stage of either operand
+        unsigned char* const to = smem + buf * kStage + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < XI; ++i) {
+            const uint32_t off = xo[i];                    // (a named value: an expression in the builtin's argument list loses the host stub)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(to + i * (WAVES * 1024)), 16, off, 0, 0, 0);
+            xo[i] += 1024;
+        }
+#pragma unroll
+        for (int i = 0; i < WI; ++i) {
+            const uint32_t off = wo[i];
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(to + (MT + i * WAVES) * 1024), 16, off, 0, 0, 0);
+            wo[i] += W_TILED ? 1024 : 64;
+        }
+    };
+    intx4 acc[UM][UN];
+#pragma unroll
+    for (int i = 0; i < UM; ++i)
+#pragma unroll
+        for (int j = 0; j < UN; ++j) acc[i][j] = intx4{0, 0, 0, 0};
+    const int x_at = wm * UM * 1024 + lane * 16;
+    const int w_at = (MT + wn * UN) * 1024 + (W_TILED ? lane * 16 : l16 * 64 + ((g ^ ((l16 / 2) & 3)) << 4));
+#pragma unroll
+    for (int s = 0; s < STAGES - 1; ++s) issue(s);
+    int buf = 0, next = STAGES - 1;
+    for (int t = 0; t < P.n_tiles; ++t) {
+        // the stages behind this one may still be on their way
+        static_assert((STAGES - 2) * (XI + WI) <= 15, "");
+        __builtin_amdgcn_s_waitcnt(0x0f70 | ((STAGES - 2) * (XI + WI)));       // vmcnt alone
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        issue(next);                                       // into the buffer that the last stage was read from
+        const unsigned char* const from = smem + buf * kStage;
+        intx4 x[UM], w[UN];
+#pragma unroll
+        for (int j = 0; j < UN; ++j) w[j] = *reinterpret_cast<const intx4*>(from + w_at + j * 1024);
+#pragma unroll
+        for (int i = 0; i < UM; ++i) x[i] = *reinterpret_cast<const intx4*>(from + x_at + i * 1024);
+#pragma unroll
+        for (int i = 0; i < UM; ++i)
+#pragma unroll
+            for (int j = 0; j < UN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i], acc[i][j], 0, 0, 0);
+        buf = buf + 1 == STAGES ? 0 : buf + 1;
+        next = next + 1 == STAGES ? 0 : next + 1;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the loads behind the last stage end before the workgroup does
+    const bool vec = P.cout % 4 == 0 && reinterpret_cast<uintptr_t>(P.out) % (4 * sizeof(T)) == 0;
+#pragma unroll
+    for (int j = 0; j < UN; ++j) {
+        const int o = o0 + (wn * UN + j) * 16 + g * 4;
+        if (o >= P.cout) continue;
+        floatx4 sw, bias{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = min(o + e, P.cout - 1);
+            sw[e] = P.sw[c];
+            if (P.bias) bias[e] = P.bias[c];
+        }
+#pragma unroll
+        for (int i = 0; i < UM; ++i) {
+            const int row = (m0 + wm * UM + i) * 16 + l16;
+            if (row >= P.n_rows) continue;
+            const float sx = P.sx[row];
+            T v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = to_out<T>(finish(acc[i][j][e], sw[e], sx, bias[e], P.relu));
+            T* const out = static_cast<T*>(P.out) + (size_t)row * P.cout + o;
+            if (vec) __builtin_memcpy(__builtin_assume_aligned(out, 4 * sizeof(T)), v, sizeof v);
+            else
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (o + e < P.cout) out[e] = v[e];
+        }
+    }
+}
+
+template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool W_TILED>
+hipError_t gemm_launch(const FcI8& P, hipStream_t st) {
+    constexpr unsigned lds = STAGES * (MT + NT) * 1024;
+    auto kernel = fc_i8_gemm_kernel<T, MT, NT, WM, WN, STAGES, W_TILED>;
+    static std::atomic<bool> raised{false};      // per instantiation
+    if (lds > 64 * 1024 && !raised.load()) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+        raised.store(true);
+    }
+    const size_t wgs = ((size_t)P.n_rows + MT * 16 - 1) / (MT * 16) * (((size_t)P.cout + NT * 16 - 1) / (NT * 16));
+    if (wgs > 0x7fffffffu) return hipErrorInvalidValue;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(WM * WN * 64), lds, st, P);
+    return hipGetLastError();
+}
+template <typename T, int MT, int NT, int WM, int WN, int STAGES>
+hipError_t gemm(const FcI8& P, bool w_tiled, hipStream_t st) {
+    return w_tiled ? gemm_launch<T, MT, NT, WM, WN, STAGES, true>(P, st) : gemm_launch<T, MT, NT, WM, WN, STAGES, false>(P, st);
+}
+
+// [cout][K] -> tiles, K padded with zeros, the last tile's missing rows left out
+__global__ __launch_bounds__(256) void tile_weights_kernel(const int8_t* __restrict__ w, int8_t* __restrict__ tiles, int K, int n_tiles, int cout) {
+    const int piece = (blockIdx.x * 256 + threadIdx.x) >> 4, r = blockIdx.y * 16 + (threadIdx.x & 15);
+    if (piece >= n_tiles * 4 || r >= cout) return;
+    *reinterpret_cast<intx4*>(tiles + tile_offset(r, piece * 16, n_tiles)) = weights16(w + (size_t)r * K, piece * 16, K);
+}
+
 template <typename T>
-hipError_t product(const FcI8& P, hipStream_t st) {
+hipError_t product(const FcI8& P, int8_t* w_tiles, hipStream_t st) {
     const dim3 block(kI8Waves * 64);
     const unsigned gx = (unsigned)((P.cout + 15) / 16);
     if (P.n_rows <= 16)
         hipLaunchKernelGGL((fc_i8_rows_kernel<T, 1>), dim3(gx, 1), block, 0, st, P);
-    else
-        hipLaunchKernelGGL((fc_i8_rows_kernel<T, 4>), dim3(gx, (unsigned)((P.n_rows + 63) / 64)), block, 0, st, P);
+    else if (P.n_rows <= kI8FewRows)
+        hipLaunchKernelGGL((fc_i8_rows_kernel<T, 4>), dim3(gx, 1), block, 0, st, P);
+    else {
+        FcI8 Q = P;
+        if (w_tiles) {
+            hipLaunchKernelGGL(tile_weights_kernel, dim3((unsigned)((P.n_tiles * 4 + 15) / 16), gx), dim3(256), 0, st, P.w, w_tiles, P.K, P.n_tiles, P.cout);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+            Q.w = w_tiles;
+        }
+        const long big = ((long)P.n_rows + 255) / 256 * ((P.cout + 255) / 256), mid = ((long)P.n_rows + 127) / 128 * ((P.cout + 127) / 128);
+        if (big >= 192) return gemm<T, 16, 16, 2, 4, 4>(Q, w_tiles != nullptr, st);
+        if (mid >= 192) return gemm<T, 8, 8, 2, 2, 4>(Q, w_tiles != nullptr, st);
+        return gemm<T, 4, 4, 2, 2, 4>(Q, w_tiles != nullptr, st);
+    }
     return hipGetLastError();
 }
 
@@ -244,22 +408,33 @@ hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, 
                             : quantize<float, false>((const float*)x, n_rows, K, q, scales, st);
 }
 
-size_t fc_i8_workspace(int n_rows, int K) {
-    const size_t rows = ((size_t)n_rows + 15) / 16 * 16;
-    return align_up(rows * ((K + 63) / 64) * 64, 256) + align_up((size_t)n_rows * sizeof(float), 256);
+// The workspace: the rows in tiles, their scales, the weights in tiles.
+struct I8Space { size_t rows, scales, weights, end; };
+static I8Space i8_space(int n_rows, int K, int cout) {
+    const size_t row = ((size_t)K + 63) / 64 * 64;
+    I8Space s;
+    s.rows = 0;
+    s.scales = align_up(align_up(n_rows, 16) * row, 256);
+    s.weights = s.scales + align_up((size_t)n_rows * sizeof(float), 256);
+    s.end = s.weights + (n_rows > kI8FewRows ? align_up(align_up(cout, 16) * row, 256) : 0);
+    return s;
 }
+size_t fc_i8_workspace(int n_rows, int K, int cout) { return i8_space(n_rows, K, cout).end; }
 
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
                         int dtype, void* ws, hipStream_t st) {
     FcI8 P;
     P.n_rows = n_rows; P.K = K; P.n_tiles = (K + 63) / 64; P.cout = cout; P.relu = relu;
-    int8_t* const xq = static_cast<int8_t*>(ws);
-    float* const sx = reinterpret_cast<float*>(xq + align_up(((size_t)n_rows + 15) / 16 * 16 * P.n_tiles * 64, 256));
-    P.xq = xq; P.sx = sx; P.w = w; P.sw = sw; P.bias = bias; P.out = out;
-    const hipError_t e = dtype == DC_BF16 ? quantize<__hip_bfloat16, true>((const __hip_bfloat16*)x, n_rows, K, xq, sx, st)
-                                          : quantize<float, true>((const float*)x, n_rows, K, xq, sx, st);
+    const I8Space space = i8_space(n_rows, K, cout);
+    int8_t* const base = static_cast<int8_t*>(ws);
+    float* const sx = reinterpret_cast<float*>(base + space.scales);
+    P.xq = base; P.sx = sx; P.w = w; P.sw = sw; P.bias = bias; P.out = out;
+    const hipError_t e = dtype == DC_BF16 ? quantize<__hip_bfloat16, true>((const __hip_bfloat16*)x, n_rows, K, base, sx, st)
+                                          : quantize<float, true>((const float*)x, n_rows, K, base, sx, st);
     if (e != hipSuccess) return e;
-    return dtype == DC_BF16 ? product<__hip_bfloat16>(P, st) : product<float>(P, st);
+    const bool whole = K % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
+    int8_t* const w_tiles = whole ? nullptr : base + space.weights;
+    return dtype == DC_BF16 ? product<__hip_bfloat16>(P, w_tiles, st) : product<float>(P, w_tiles, st);
 }
 
 }  // namespace dc

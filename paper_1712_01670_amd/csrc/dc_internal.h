@@ -196,7 +196,7 @@ hipError_t launch_fc(const void* x, const void* w, const float* bias, void* out,
 constexpr size_t kI8MaxK = 131072;       // 127 * 127 * K < 2^31
 // q [n_rows][K], scales [n_rows]
 hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, int8_t* q, float* scales, hipStream_t st);
-size_t fc_i8_workspace(int n_rows, int K);
+size_t fc_i8_workspace(int n_rows, int K, int cout);
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
                         int dtype, void* ws, hipStream_t st);
 // ---- mixture-of-experts layer (dc_moe.hip) ----
