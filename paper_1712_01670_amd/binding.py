@@ -7,6 +7,7 @@ loudly if it has not been built.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import threading
 import types
@@ -159,6 +160,11 @@ def _stream():
     return C.c_void_p(torch.cuda.current_stream().cuda_stream)
 
 
+def _raw_stream(device):
+    """The current stream of a cuda device as _stream gives it, without the object around it (3 us a call)."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
 def _ptr(t):
     return C.c_void_p(t.data_ptr()) if t is not None else None
 
@@ -179,6 +185,7 @@ class _Here:
 
 
 _HERE_DEVICE = _Here()
+_ROW_TYPES = {torch.float32: DC_F32, torch.bfloat16: DC_BF16}
 
 
 def _on(device):
@@ -188,19 +195,32 @@ def _on(device):
 
 def _rows_dtype(fn, x):
     """DC_F32 or DC_BF16 of a contiguous cuda tensor of rows; anything else is an error."""
+    dtype = _ROW_TYPES.get(x.dtype)
+    if dtype is None:
+        raise ValueError(f"{fn}: {x.dtype} rows (float32 or bfloat16)")
     if not x.is_cuda or not x.is_contiguous() or x.dim() < 1:
         raise ValueError(f"{fn}: the rows have to be a contiguous cuda tensor")
-    if x.dtype == torch.bfloat16:
-        return DC_BF16
-    if x.dtype != torch.float32:
-        raise ValueError(f"{fn}: {x.dtype} rows (float32 or bfloat16)")
-    return DC_F32
+    return dtype
 
 
 def _want(fn, t, dtype, shape, device):
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{fn}: wants a contiguous {dtype} {tuple(shape)} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{fn}: wants a contiguous {dtype} {shape} on {device}, got {t.dtype} {tuple(t.shape)} on {t.device}"
                          + ("" if t.is_contiguous() else ", not contiguous"))
+
+
+@functools.lru_cache(maxsize=256)
+def _fc_quant_bytes(n, K, cout):
+    need = C.c_size_t()
+    _check("dc_fc_quant_workspace_bytes", lib().dc_fc_quant_workspace_bytes(n, K, cout, C.byref(need)))
+    return need.value
+
+
+@functools.lru_cache(maxsize=256)
+def _moe_bytes(*fields):
+    need = C.c_size_t()
+    _check("dc_moe_workspace_bytes", lib().dc_moe_workspace_bytes(C.byref(Moe(*fields[:-1])), fields[-1], C.byref(need)))
+    return need.value
 
 
 def _scratch(n_bytes, device):
@@ -563,14 +583,13 @@ def dc_fc_quant_layer(x, weights, scales, bias, relu):
     _want("dc_fc_quant_layer", scales, torch.float32, (cout,), x.device)
     if bias is not None:
         _want("dc_fc_quant_layer", bias, torch.float32, (cout,), x.device)
-    out = torch.empty((n, 1, 1, cout), dtype=x.dtype, device=x.device)
+    need = _fc_quant_bytes(n, K, cout)
     with _on(x.device):
-        need = C.c_size_t()
-        _check("dc_fc_quant_workspace_bytes", lib().dc_fc_quant_workspace_bytes(n, K, cout, C.byref(need)))
-        ws = _scratch(need.value, x.device)
+        out = x.new_empty((n, 1, 1, cout))
+        ws = _scratch(need, x.device)
         _check("dc_fc_quant_layer", lib().dc_fc_quant_layer(
             x.data_ptr(), weights.data_ptr(), scales.data_ptr(), None if bias is None else bias.data_ptr(), out.data_ptr(), n, K, cout,
-            int(relu), dtype, None if ws is None else ws.data_ptr(), need.value, _stream()))
+            int(relu), dtype, None if ws is None else ws.data_ptr(), need, _raw_stream(x.device)))
     return out
 
 
@@ -594,16 +613,15 @@ def dc_moe_layer(moe, x, router, up, down, router_bias=None, up_bias=None, down_
         if t is not None:
             _want(fn, t, torch.float32, shape, dev)
     m = Moe(E, k, cin, hidden, cout, act, int(moe["renormalize"]), DC_I8 if int8 else dtype)
+    need = _moe_bytes(E, k, cin, hidden, cout, act, m.renormalize, m.wtype, n)
     p = [t.data_ptr() if t is not None else None for t in (router, router_bias, up, up_scale, up_bias, down, down_scale, down_bias)]
-    out = torch.empty((n, cout), dtype=x.dtype, device=dev)
-    experts = torch.empty((n, k), dtype=torch.int32, device=dev)
-    gates = torch.empty((n, k), dtype=torch.float32, device=dev)
     with _on(dev):
-        need = C.c_size_t()
-        _check("dc_moe_workspace_bytes", lib().dc_moe_workspace_bytes(C.byref(m), n, C.byref(need)))
-        ws = _scratch(need.value, dev)
+        out = x.new_empty((n, cout))
+        experts = torch.empty((n, k), dtype=torch.int32, device=dev)
+        gates = torch.empty((n, k), dtype=torch.float32, device=dev)
+        ws = _scratch(need, dev)
         _check(fn, lib().dc_moe_layer(C.byref(m), C.byref(MoeWeights(*p)), x.data_ptr(), out.data_ptr(), experts.data_ptr(), gates.data_ptr(),
-                                      n, dtype, ws.data_ptr(), need.value, _stream()))
+                                      n, dtype, ws.data_ptr(), need, _raw_stream(dev)))
     return out, experts, gates
 
 

@@ -31,71 +31,142 @@ __device__ __forceinline__ int quotient8(float x, float s, float inv) {
     else if (r2 < -s || (r2 == -s && odd)) q -= 1.f;
     return (int)fminf(fmaxf(q, -127.f), 127.f);      // (a scale among the subnormal numbers is coarse: more than 127 of it fit)
 }
-
-template <typename T>
-struct In16;                                         // 16 elements of a row
-template <>
-struct In16<float> {
-    typedef float vec_any __attribute__((ext_vector_type(4), aligned(4)));
-    static __device__ __forceinline__ void load(const float* p, float (&f)[16]) {
+// N of them, as bytes.  x times 1 / s is within 8e-6 of the quotient (1 / s is off by half a step, the product goes into the sum
+// unrounded, and the quotient is 127 at most), so its nearest integer is the right one unless it lies that close to the border:
+// then, for one vector of a wavefront in a hundred, the exact form above decides.  Adding 1.5 * 2^23 rounds to an integer, whose
+// low byte is the result.
+constexpr float kRound = 12582912.f;
+template <int N>
+__device__ __forceinline__ void quotients8(const float (&x)[N], float s, float inv, uint32_t (&v)[N / 4]) {
+    uint32_t r[N];
+    float off = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const vec_any v = *reinterpret_cast<const vec_any*>(p + 4 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) f[4 * i + e] = v[e];
-        }
+    for (int e = 0; e < N; ++e) {
+        const float t = fmaf(x[e], inv, kRound);
+        r[e] = __float_as_uint(t);
+        off = fmaxf(off, fabsf(fmaf(x[e], inv, kRound - t)));
     }
-    static __device__ __forceinline__ float one(const float* p) { return *p; }
-};
-template <>
-struct In16<__hip_bfloat16> {
-    typedef uint32_t vec_any __attribute__((ext_vector_type(4), aligned(2)));
-    static __device__ __forceinline__ void load(const __hip_bfloat16* p, float (&f)[16]) {
+    if (!(off < 0.49999f && s >= 0x1p-100f)) {
+        const float up = s < 0x1p-100f ? 0x1p64f : 1.f;      // keeps 1 / s finite; a power of two changes no quotient
+        const float su = s * up, iu = 1.f / su;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const vec_any v = *reinterpret_cast<const vec_any*>(p + 8 * i);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f[8 * i + 2 * e] = __uint_as_float(v[e] << 16);
-                f[8 * i + 2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
-            }
-        }
+        for (int e = 0; e < N; ++e) r[e] = (uint32_t)quotient8(x[e] * up, su, iu);
     }
-    static __device__ __forceinline__ float one(const __hip_bfloat16* p) { return __bfloat162float(*p); }
-};
-
-// Rows for the matrix units: tiles of 16 rows x 64 bytes in the order of a fragment's lanes (lane l: row l % 16, bytes
-// 16 (l / 16) on), 1 KiB in one piece, K padded with zeros to whole tiles.  Tile (i, j) is number i * n_tiles + j.
-__device__ __forceinline__ size_t tile_offset(size_t row, int k0, int n_tiles) {
-    return ((row >> 4) * n_tiles + (k0 >> 6)) * 1024 + ((k0 >> 4) & 3) * 256 + (row & 15) * 16;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        const uint32_t lo = __builtin_amdgcn_perm(r[4 * i + 1], r[4 * i], 0x0c0c0400u), hi = __builtin_amdgcn_perm(r[4 * i + 3], r[4 * i + 2], 0x0c0c0400u);
+        v[i] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+    }
 }
 
-// LANES threads share a row and hold it in registers, CH pieces of 16 elements each, so it is read once.
-// TILED: the layout above; otherwise [n_rows][K].
+// 16 bytes of a row as fp32, at any address its type allows; zeros behind the row's end.
+template <typename T>
+struct RowVec;
+template <>
+struct RowVec<float> {
+    static constexpr int N = 4;
+    typedef uint32_t any __attribute__((ext_vector_type(4), aligned(4)));
+    static __device__ __forceinline__ float one(const float* p) { return *p; }
+    static __device__ __forceinline__ void load(const float* p, float (&f)[4]) {
+        const any v = *reinterpret_cast<const any*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) f[e] = __uint_as_float(v[e]);
+    }
+};
+template <>
+struct RowVec<__hip_bfloat16> {
+    static constexpr int N = 8;
+    typedef uint32_t any __attribute__((ext_vector_type(4), aligned(2)));
+    static __device__ __forceinline__ float one(const __hip_bfloat16* p) { return __bfloat162float(*p); }
+    static __device__ __forceinline__ void load(const __hip_bfloat16* p, float (&f)[8]) {
+        const any v = *reinterpret_cast<const any*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            f[2 * e] = __uint_as_float(v[e] << 16);
+            f[2 * e + 1] = __uint_as_float(v[e] & 0xffff0000u);
+        }
+    }
+};
+template <typename T, int N>
+__device__ __forceinline__ void load_row(const T* row, int k0, int K, float (&f)[N]) {
+    if (k0 + N <= K) {
+        RowVec<T>::load(row + k0, f);
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e) f[e] = k0 + e < K ? RowVec<T>::one(row + k0 + e) : 0.f;
+    }
+}
+
+// What the bits of a row's largest |x| make of it.
+struct RowScale {
+    float scale, s, inv;
+    bool zero;
+    __device__ __forceinline__ explicit RowScale(uint32_t top) {
+        const bool bad = top >= 0x7f800000u;
+        s = __uint_as_float(top) / 127.f;
+        scale = bad ? __uint_as_float(0x7fc00000u) : s;
+        zero = bad || !(s > 0.f);
+        inv = 1.f / s;
+    }
+};
+
+// Where a row's bytes go: [n_rows][stride], `width` of them (zeros behind K); or tiles of 16 rows x 64 bytes in the order of a
+// fragment's lanes (lane l: row l % 16, bytes 16 (l / 16) on), 1 KiB in one piece, tile (i, j) being number i * n_tiles + j.
+struct Rows8 { int8_t* q; size_t stride; int width; };
+__device__ __forceinline__ size_t tile_offset(size_t row, int k0, int n_tiles) {
+    return ((row >> 4) * n_tiles + (k0 >> 6)) * 1024 + ((k0 >> 4) & 3) * 256 + (row & 15) * 16 + (k0 & 15);
+}
+template <bool TILED, int N>
+__device__ __forceinline__ void store8(const Rows8& to, size_t row, int k0, const uint32_t (&v)[N / 4]) {
+    typedef uint32_t any __attribute__((ext_vector_type(N / 4), aligned(TILED ? N : 1)));
+    any w;
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) w[i] = v[i];
+    if constexpr (TILED) {
+        *reinterpret_cast<any*>(to.q + tile_offset(row, k0, to.width >> 6)) = w;
+    } else if (k0 + N <= to.width) {
+        *reinterpret_cast<any*>(to.q + row * to.stride + k0) = w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (k0 + e < to.width) to.q[row * to.stride + k0 + e] = (int8_t)(v[e >> 2] >> (8 * (e & 3)));
+    }
+}
+
+// LANES threads share a row, a vector each and LANES vectors further the next.  CH > 0: they hold the row in registers, so it is
+// read once; CH == 0: a row that is too long for that is read twice, the second time from the cache.
 template <typename T, int LANES, int CH, bool TILED>
-__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void quantize_rows_kernel(const T* __restrict__ x, size_t n_rows, int K, int n_tiles,
-                                                                                  int8_t* __restrict__ q, float* __restrict__ scales) {
-    constexpr int THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES;
+__global__ __launch_bounds__(LANES > 256 ? LANES : 256) void quantize_rows_kernel(const T* __restrict__ x, size_t n_rows, int K, Rows8 to,
+                                                                                  float* __restrict__ scales) {
+    constexpr int THREADS = LANES > 256 ? LANES : 256, ROWS = THREADS / LANES, N = RowVec<T>::N;
     const int tid = threadIdx.x, part = tid % LANES;
     const size_t row = (size_t)blockIdx.x * ROWS + tid / LANES;
     const bool live = row < n_rows;
     const T* const xr = x + (live ? row : 0) * K;
-    float f[CH][16];
+    const int vecs = live ? (to.width + N - 1) / N : 0;
+    float f[CH ? CH : 1][N];
     uint32_t top = 0;                                // the largest |x|: as whole numbers, infinities and NaN come out on top
+    auto look = [&](const float (&v)[N]) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int k0 = (c * LANES + part) * 16;
-        if (live && k0 + 16 <= K) {
-            In16<T>::load(xr + k0, f[c]);
-        } else {
+        for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+    };
+    if constexpr (CH > 0) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) f[c][e] = live && k0 + e < K ? In16<T>::one(xr + k0 + e) : 0.f;
+        for (int c = 0; c < CH; ++c)
+            if (c * LANES + part < vecs) {
+                load_row(xr, (c * LANES + part) * N, K, f[c]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[c][e] = 0.f;
+            }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) look(f[c]);
+    } else {
+        for (int i = part; i < vecs; i += LANES) {
+            load_row(xr, i * N, K, f[0]);
+            look(f[0]);
         }
     }
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = max(top, __float_as_uint(f[c][e]) & 0x7fffffffu);
 #pragma unroll
     for (int d = (LANES < 64 ? LANES : 64) / 2; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
     if constexpr (LANES > 64) {
@@ -107,58 +178,60 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void quantize_rows_kerne
         for (int i = 0; i < LANES / 64; ++i) top = max(top, tops[first + i]);
     }
     if (!live) return;
-    const bool bad = top >= 0x7f800000u;
-    const float s = __uint_as_float(top) / 127.f;
-    if (part == 0) scales[row] = bad ? __uint_as_float(0x7fc00000u) : s;
-    const bool zero = bad || !(s > 0.f);
-    const float up = s < 0x1p-100f ? 0x1p64f : 1.f;  // keeps 1 / s finite; a power of two changes no quotient
-    const float su = s * up, inv = 1.f / su;
+    const RowScale s(top);
+    if (part == 0) scales[row] = s.scale;
+    auto put = [&](int i, const float (&v)[N]) {
+        uint32_t w[N / 4] = {};
+        if (!s.zero) quotients8(v, s.s, s.inv, w);
+        store8<TILED, N>(to, row, i * N, w);
+    };
+    if constexpr (CH > 0) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-        const int k0 = (c * LANES + part) * 16;
-        intx4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t w = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) w |= (uint32_t)(quotient8(f[c][4 * i + e] * up, su, inv) & 255) << (8 * e);
-            v[i] = zero ? 0 : (int)w;
-        }
-        if constexpr (TILED) {
-            if (k0 < n_tiles * 64) *reinterpret_cast<intx4*>(q + tile_offset(row, k0, n_tiles)) = v;
-        } else if (k0 + 16 <= K) {
-            *reinterpret_cast<intx4_any*>(q + row * K + k0) = v;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                if (k0 + e < K) q[row * K + k0 + e] = (int8_t)((uint32_t)v[e >> 2] >> (8 * (e & 3)));
+        for (int c = 0; c < CH; ++c)
+            if (c * LANES + part < vecs) put(c * LANES + part, f[c]);
+    } else {
+        for (int i = part; i < vecs; i += LANES) {
+            load_row(xr, i * N, K, f[0]);
+            put(i, f[0]);
         }
     }
 }
 
 template <typename T, bool TILED>
-hipError_t quantize(const T* x, size_t n_rows, int K, int8_t* q, float* scales, hipStream_t st) {
-    const int n_tiles = (K + 63) / 64;
+hipError_t quantize(const T* x, size_t n_rows, int K, const Rows8& to, float* scales, hipStream_t st) {
     auto go = [&](auto lanes, auto ch) {
         constexpr int LANES = decltype(lanes)::value, CH = decltype(ch)::value, THREADS = LANES > 256 ? LANES : 256;
         const size_t wgs = (n_rows + THREADS / LANES - 1) / (THREADS / LANES);
-        hipLaunchKernelGGL((quantize_rows_kernel<T, LANES, CH, TILED>), dim3((unsigned)wgs), dim3(THREADS), 0, st, x, n_rows, K, n_tiles, q, scales);
+        hipLaunchKernelGGL((quantize_rows_kernel<T, LANES, CH, TILED>), dim3((unsigned)wgs), dim3(THREADS), 0, st, x, n_rows, K, to, scales);
         return hipGetLastError();
     };
     using std::integral_constant;
-    const int pieces = n_tiles * 4;
-    if (pieces <= 64) return go(integral_constant<int, 16>(), integral_constant<int, 4>());
-    if (pieces <= 256) return go(integral_constant<int, 64>(), integral_constant<int, 4>());
-    if (pieces <= 1024) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
-    if (pieces <= 4096) return go(integral_constant<int, 1024>(), integral_constant<int, 4>());
-    return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
+    const int vecs = (to.width + RowVec<T>::N - 1) / RowVec<T>::N;
+    // a vector or two a thread is the shortest way through a row; many rows want up to four, whose loads travel together, and few
+    // lanes, whose sums are cheap (12544 rows of 1024 bf16: 16 x 8 8.7 us, 32 x 4 7.9, 128 x 4 11.0, 256 x 1 12.4; 50176 of 256: 16 x 4
+    // 8.4, 64 x 2 15.4, 256 x 1 33.5)
+    if (n_rows < 2048) {
+        if (vecs <= 128) return go(integral_constant<int, 64>(), integral_constant<int, 2>());
+        if (vecs <= 512) return go(integral_constant<int, 256>(), integral_constant<int, 2>());
+    } else if constexpr (!TILED) {
+        if (vecs <= 64) return go(integral_constant<int, 16>(), integral_constant<int, 4>());
+        if (vecs <= 128) return go(integral_constant<int, 32>(), integral_constant<int, 4>());
+        if (vecs <= 256) return go(integral_constant<int, 64>(), integral_constant<int, 4>());
+        if (vecs <= 512) return go(integral_constant<int, 128>(), integral_constant<int, 4>());
+        if (vecs <= 1024) return go(integral_constant<int, 256>(), integral_constant<int, 4>());
+    }
+    if (vecs <= 2048) return go(integral_constant<int, 1024>(), integral_constant<int, 2>());
+    if (vecs <= 8192) return go(integral_constant<int, 1024>(), integral_constant<int, 8>());
+    return go(integral_constant<int, 1024>(), integral_constant<int, 0>());
 }
 
 // ---- the product ------------------------------------------------------------------------------------------------------
 struct FcI8 {
-    const int8_t* xq;          // rows in tiles
+    const void* x;             // [n_rows][K] in the storage type
+    const int8_t* xq;          // rows: in tiles for the kernel of few rows, [n_rows][x_stride] for the GEMM
+    size_t x_stride, w_stride;
     const float* sx;
-    const int8_t* w;           // [cout][K]
+    const int8_t* w;           // [cout][w_stride]
     const float* sw;
     const float* bias;
     void* out;
@@ -186,42 +259,131 @@ __device__ __forceinline__ intx4 weights16(const int8_t* __restrict__ row, int k
     return v;
 }
 
-// A workgroup takes 16 channels x NB * 16 rows; its wavefronts deal the tiles of K among themselves and add their integer
-// sums through LDS.
-constexpr int kI8Waves = 8;
 constexpr int kI8FewRows = 64;
-template <typename T, int NB>
-__global__ __launch_bounds__(kI8Waves * 64) void fc_i8_rows_kernel(FcI8 P) {
-    __shared__ intx4 red[kI8Waves][NB][64];
+
+// Few rows: a workgroup takes 16 channels x NB * 16 rows.  Its wavefronts deal the 128-byte steps of K among themselves and add
+// their integer sums through LDS.  The weights are what has to come from memory: they go straight from there into fragments
+// (16 rows of 64 bytes an instruction), AHEAD steps of a wavefront before they are multiplied.  The rows come from L2, in tiles.
+// OWN: there is one row, and every workgroup rounds it itself, into LDS, while its first weights travel, which saves a launch
+// (9216 -> 4096: 9.3 us against 8.6 + 3.1; four rows that way 15.0 against 8.6 + 3.1).
+template <typename T, int NB, int WAVES, int AHEAD, bool OWN>
+__global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
+    static_assert(!OWN || NB == 1, "");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
-    const int o0 = blockIdx.x * 16, r0 = blockIdx.y * (NB * 16);
+    const int o0 = blockIdx.x * 16;
     // channels past the end repeat the last one (not stored)
     const int8_t* const wrow = P.w + (size_t)min(o0 + l16, P.cout - 1) * P.K;
-    const int n_blocks = min(NB, (P.n_rows - r0 + 15) / 16);
-    const int8_t* const xt = P.xq + (size_t)(r0 >> 4) * P.n_tiles * 1024 + lane * 16;
+    const int steps = P.n_tiles / 2, whole = P.K / 128;
+    struct Step { intx4 w[2], x[OWN ? 1 : NB][2]; };
+    const int8_t* const xt = P.xq + lane * 16;
+    auto fetch = [&](Step& b, int s) {
+        if (s < whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b.w[h] = *reinterpret_cast<const intx4_any*>(wrow + s * 128 + h * 64 + g * 16);
+        } else if (s < steps) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b.w[h] = weights16(wrow, s * 128 + h * 64 + g * 16, P.K);
+        }
+        if constexpr (!OWN) {
+            if (s < steps)
+#pragma unroll
+                for (int j = 0; j < NB; ++j)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) b.x[j][h] = *reinterpret_cast<const intx4*>(xt + ((size_t)j * P.n_tiles + s * 2 + h) * 1024);
+        }
+    };
+    Step step[AHEAD + 1];
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d) fetch(step[d], wave + d * WAVES);
+    __builtin_amdgcn_sched_barrier(0);
+    unsigned char* const own_x = smem + 256;               // [width], behind the wavefronts' largest |x|
+    float own_scale = 0.f;
+    if constexpr (OWN) {
+        constexpr int N = RowVec<T>::N, THREADS = WAVES * 64, CH = 4;
+        const T* const x = static_cast<const T*>(P.x);
+        const int vecs = P.n_tiles * 64 / N;
+        float f[CH][N];                                    // (what does not fit is read again)
+        uint32_t top = 0;
+        auto look = [&](const float (&v)[N]) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) top = max(top, __float_as_uint(v[e]) & 0x7fffffffu);
+        };
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (c * THREADS + tid < vecs) {
+                load_row(x, (c * THREADS + tid) * N, P.K, f[c]);
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[c][e] = 0.f;
+            }
+#pragma unroll
+        for (int c = 0; c < CH; ++c) look(f[c]);
+        for (int i = CH * THREADS + tid; i < vecs; i += THREADS) {
+            float more[N];
+            load_row(x, i * N, P.K, more);
+            look(more);
+        }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+        uint32_t* const tops = reinterpret_cast<uint32_t*>(smem);
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) top = max(top, tops[v]);
+        const RowScale s(top);
+        own_scale = s.scale;
+        auto put = [&](int i, const float (&v)[N]) {
+            uint32_t w[N / 4] = {};
+            if (!s.zero) quotients8(v, s.s, s.inv, w);
+#pragma unroll
+            for (int e = 0; e < N / 4; ++e) reinterpret_cast<uint32_t*>(own_x)[i * (N / 4) + e] = w[e];
+        };
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (c * THREADS + tid < vecs) put(c * THREADS + tid, f[c]);
+        for (int i = CH * THREADS + tid; i < vecs; i += THREADS) {
+            float more[N];
+            load_row(x, i * N, P.K, more);
+            put(i, more);
+        }
+        __syncthreads();
+    }
     intx4 acc[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) acc[j] = intx4{0, 0, 0, 0};
-    for (int t = wave; t < P.n_tiles; t += kI8Waves) {
-        const intx4 wv = weights16(wrow, t * 64 + g * 16, P.K);
+    for (int s = wave; s < steps; s += (AHEAD + 1) * WAVES) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
-            if (j < n_blocks) {
-                const intx4 xv = *reinterpret_cast<const intx4*>(xt + ((size_t)j * P.n_tiles + t) * 1024);
-                acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wv, xv, acc[j], 0, 0, 0);
-            }
+        for (int d = 0; d <= AHEAD; ++d) {
+            if (s + d * WAVES >= steps) break;
+            fetch(step[(d + AHEAD) % (AHEAD + 1)], s + (d + AHEAD) * WAVES);
+            __builtin_amdgcn_sched_barrier(0);
+            const Step& b = step[d];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    intx4 x;
+                    if constexpr (OWN) x = *reinterpret_cast<const intx4*>(own_x + (s + d * WAVES) * 128 + h * 64 + g * 16);
+                    else x = b.x[j][h];
+                    acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.w[h], x, acc[j], 0, 0, 0);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
+    if constexpr (OWN) __syncthreads();                    // the row has been read
+    intx4* const red = reinterpret_cast<intx4*>(smem + 256);               // [WAVES][NB][64]
 #pragma unroll
-    for (int j = 0; j < NB; ++j) red[wave][j][lane] = acc[j];
+    for (int j = 0; j < NB; ++j) red[(wave * NB + j) * 64 + lane] = acc[j];
     __syncthreads();
-    for (int i = tid; i < NB * 64; i += kI8Waves * 64) {
-        const int j = i >> 6, l = i & 63, row = r0 + j * 16 + (l & 15), o = o0 + (l >> 4) * 4;
+    for (int i = tid; i < NB * 64; i += WAVES * 64) {
+        const int l = i & 63, row = (i >> 6) * 16 + (l & 15), o = o0 + (l >> 4) * 4;
         if (row >= P.n_rows || o >= P.cout) continue;
-        intx4 sum = red[0][j][l];
+        intx4 sum = red[i];
 #pragma unroll
-        for (int v = 1; v < kI8Waves; ++v) sum += red[v][j][l];
-        const float sx = P.sx[row];
+        for (int v = 1; v < WAVES; ++v) sum += red[v * NB * 64 + i];
+        const float sx = OWN ? own_scale : P.sx[row];
         T* const out = static_cast<T*>(P.out) + (size_t)row * P.cout;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -231,21 +393,22 @@ __global__ __launch_bounds__(kI8Waves * 64) void fc_i8_rows_kernel(FcI8 P) {
     }
 }
 
-// Many rows: a GEMM of MT * 16 rows x NT * 16 channels per workgroup.  Both operands come through LDS in stages of 64 bytes of K
-// by direct loads, STAGES - 1 of them on their way while one is multiplied; a barrier a stage.  A wavefront's part is
-// MT / WM row tiles x NT / WN channel tiles, which is what a fragment read from LDS serves.
-// The rows are tiles as they are (fragments of 1 KiB: no bank is asked twice).  Weights come from [cout][K] when their rows are
-// whole aligned vectors (an instruction brings 16 rows of 64 bytes, four lanes a row; the four vectors of row r are stored in the
-// order v ^ (r / 2 % 4), so that eight neighbouring fragment lanes ask 128 different bytes), otherwise from a copy in
-// tiles (W_TILED).  What lies behind the end of a row of weights meets zeros of the input row; what lies behind an operand's
-// end reads as zero.
+// Many rows: a GEMM of MT * 16 rows x NT * 16 channels per workgroup.  Both operands come through LDS in stages of 128 bytes of K
+// by direct loads: an instruction brings 8 rows of 128 bytes, whole cache lines, eight lanes a row, and the eight vectors of
+// row r are stored in the order v ^ (r % 8), so that eight neighbouring lanes of a fragment ask 128 different bytes.  Half a
+// stage is multiplied while the fragments of the next half are read into the other set of registers; one barrier a stage.
+// Rows are whole 16-byte vectors; what lies behind a row of weights meets zeros of the input row, and what lies behind an
+// operand's end reads as zero.
 constexpr int kBufferFlags = 0x00020000;
+constexpr int kMaxLds = 160 * 1024;
 typedef __attribute__((address_space(3))) void* lds_ptr;
-template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool W_TILED>
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14); }
+template <typename T, int MT, int NT, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
-    constexpr int WAVES = WM * WN, XI = MT / WAVES, WI = NT / WAVES, UM = MT / WM, UN = NT / WN;
-    static_assert(MT % WAVES == 0 && NT % WAVES == 0, "every wavefront loads as many tiles of either operand");
-    constexpr int kStage = (MT + NT) * 1024;
+    constexpr int WAVES = WM * WN, XI = 2 * MT / WAVES, WI = 2 * NT / WAVES, UM = MT / WM, UN = NT / WN;
+    static_assert(2 * MT % WAVES == 0 && 2 * NT % WAVES == 0, "every wavefront loads as many rows of either operand");
+    constexpr int kStage = (MT + NT) * 2048;
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
@@ -259,35 +422,31 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
         tm = band * 8 + in % left;
         tn = in / left;
     }
-    const int m0 = tm * MT, o0 = tn * (NT * 16);           // first row tile, first channel
-    const int m_tiles = min(MT, (P.n_rows + 15) / 16 - m0), chans = min(NT * 16, P.cout - o0);
-    const size_t tile_row = (size_t)P.n_tiles * 1024;
-    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<int8_t*>(P.xq) + m0 * tile_row, 0, (uint32_t)(m_tiles * tile_row), kBufferFlags);
-    const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(
-        const_cast<int8_t*>(P.w) + (W_TILED ? (o0 >> 4) * tile_row : (size_t)o0 * P.K), 0,
-        (uint32_t)(W_TILED ? (chans + 15) / 16 * tile_row : (size_t)chans * P.K), kBufferFlags);
+    const int m0 = tm * (MT * 16), o0 = tn * (NT * 16);    // first row, first channel
+    const int rows = min(MT * 16, P.n_rows - m0), chans = min(NT * 16, P.cout - o0);
+    const __amdgpu_buffer_rsrc_t x_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(P.xq) + m0 * P.x_stride, 0,
+                                                                            (uint32_t)(rows * P.x_stride), kBufferFlags);
+    const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(P.w) + o0 * P.w_stride, 0,
+                                                                            (uint32_t)(chans * P.w_stride), kBufferFlags);
     uint32_t xo[XI], wo[WI];
+    const int r = lane >> 3, v16 = ((lane & 7) ^ r) << 4;
 #pragma unroll
-    for (int i = 0; i < XI; ++i) xo[i] = (uint32_t)((i * WAVES + wave) * tile_row) + lane * 16;
+    for (int i = 0; i < XI; ++i) xo[i] = (uint32_t)(((i * WAVES + wave) * 8 + r) * P.x_stride) + v16;
 #pragma unroll
-    for (int i = 0; i < WI; ++i) {
-        const int t = i * WAVES + wave, r = lane >> 2;
-        wo[i] = W_TILED ? (uint32_t)(t * tile_row) + lane * 16 : (uint32_t)(t * 16 + r) * P.K + (((lane & 3) ^ ((r / 2) & 3)) << 4);
-    }
+    for (int i = 0; i < WI; ++i) wo[i] = (uint32_t)(((i * WAVES + wave) * 8 + r) * P.w_stride) + v16;
     auto issue = [&](int buf) {                            // the next stage of either operand
         unsigned char* const to = smem + buf * kStage + wave * 1024;
 #pragma unroll
         for (int i = 0; i < XI; ++i) {
             const uint32_t off = xo[i];                    // (a named value: an expression in the builtin's argument list loses the host stub)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(x_rsrc, (lds_ptr)(to + i * (WAVES * 1024)), 16, off, 0, 0, 0);
-            xo[i] += 1024;
+            xo[i] += 128;
         }
 #pragma unroll
         for (int i = 0; i < WI; ++i) {
             const uint32_t off = wo[i];
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(to + (MT + i * WAVES) * 1024), 16, off, 0, 0, 0);
-            wo[i] += W_TILED ? 1024 : 64;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(w_rsrc, (lds_ptr)(to + (MT * 2 + i * WAVES) * 1024), 16, off, 0, 0, 0);
+            wo[i] += 128;
         }
     };
     intx4 acc[UM][UN];
@@ -295,31 +454,56 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     for (int i = 0; i < UM; ++i)
 #pragma unroll
         for (int j = 0; j < UN; ++j) acc[i][j] = intx4{0, 0, 0, 0};
-    const int x_at = wm * UM * 1024 + lane * 16;
-    const int w_at = (MT + wn * UN) * 1024 + (W_TILED ? lane * 16 : l16 * 64 + ((g ^ ((l16 / 2) & 3)) << 4));
+    const int x_at = (wm * UM * 16 + l16) * 128, w_at = (MT * 16 + wn * UN * 16 + l16) * 128;
+    const int half_at[2] = {(g ^ (l16 & 7)) << 4, ((g + 4) ^ (l16 & 7)) << 4};
+    intx4 x[2][UM], w[2][UN];
+    auto fragments = [&](int half, int buf) {
+        const unsigned char* const from = smem + buf * kStage + half_at[half];
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) issue(s);
-    int buf = 0, next = STAGES - 1;
-    for (int t = 0; t < P.n_tiles; ++t) {
-        // the stages behind this one may still be on their way
-        static_assert((STAGES - 2) * (XI + WI) <= 15, "");
-        __builtin_amdgcn_s_waitcnt(0x0f70 | ((STAGES - 2) * (XI + WI)));       // vmcnt alone
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        issue(next);                                       // into the buffer that the last stage was read from
-        const unsigned char* const from = smem + buf * kStage;
-        intx4 x[UM], w[UN];
+        for (int j = 0; j < UN; ++j) w[half][j] = *reinterpret_cast<const intx4*>(from + w_at + j * 2048);
 #pragma unroll
-        for (int j = 0; j < UN; ++j) w[j] = *reinterpret_cast<const intx4*>(from + w_at + j * 1024);
-#pragma unroll
-        for (int i = 0; i < UM; ++i) x[i] = *reinterpret_cast<const intx4*>(from + x_at + i * 1024);
+        for (int i = 0; i < UM; ++i) x[half][i] = *reinterpret_cast<const intx4*>(from + x_at + i * 2048);
+    };
+    auto multiply = [&](int half) {
 #pragma unroll
         for (int i = 0; i < UM; ++i)
 #pragma unroll
-            for (int j = 0; j < UN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[j], x[i], acc[i][j], 0, 0, 0);
-        buf = buf + 1 == STAGES ? 0 : buf + 1;
-        next = next + 1 == STAGES ? 0 : next + 1;
+            for (int j = 0; j < UN; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[half][j], x[half][i], acc[i][j], 0, 0, 0);
+    };
+    // the order of a half: a fragment's read, a few products, and so on, so that the reads travel behind the products
+    constexpr int kLoads = XI + WI, kReads = UM + UN, kProducts = UM * UN;
+    auto interleave = [&]() {
+#pragma unroll
+        for (int i = 0; i < kReads; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, kProducts / kReads, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, kProducts - kProducts / kReads * kReads, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int s = 0; s < STAGES; ++s) issue(s);
+    wait_vmcnt<(STAGES - 1) * kLoads>();
+    asm volatile("s_barrier" ::: "memory");
+    fragments(0, 0);
+    int buf = 0;
+    const int stages = P.n_tiles / 2;
+    for (int t = 0; t < stages; ++t) {
+        const int next = buf + 1 == STAGES ? 0 : buf + 1;
+        fragments(1, buf);
+        multiply(0);
+        interleave();
+        wait_vmcnt<(STAGES - 2) * kLoads>();
+        // every wavefront has the rest of this stage in registers, and the next stage has arrived
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        issue(buf);
+        __builtin_amdgcn_sched_barrier(0);
+        fragments(0, next);
+        multiply(1);
+        interleave();
+        buf = next;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the loads behind the last stage end before the workgroup does
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");       // the loads behind the last stage end before the workgroup does
     const bool vec = P.cout % 4 == 0 && reinterpret_cast<uintptr_t>(P.out) % (4 * sizeof(T)) == 0;
 #pragma unroll
     for (int j = 0; j < UN; ++j) {
@@ -334,7 +518,7 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
         }
 #pragma unroll
         for (int i = 0; i < UM; ++i) {
-            const int row = (m0 + wm * UM + i) * 16 + l16;
+            const int row = m0 + (wm * UM + i) * 16 + l16;
             if (row >= P.n_rows) continue;
             const float sx = P.sx[row];
             T v[4];
@@ -350,91 +534,108 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     }
 }
 
-template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool W_TILED>
-hipError_t gemm_launch(const FcI8& P, hipStream_t st) {
-    constexpr unsigned lds = STAGES * (MT + NT) * 1024;
-    auto kernel = fc_i8_gemm_kernel<T, MT, NT, WM, WN, STAGES, W_TILED>;
-    static std::atomic<bool> raised{false};      // per instantiation
+// A kernel whose LDS is sized at the launch; the attribute is raised once per instantiation.
+template <typename K>
+hipError_t launch_lds(K kernel, std::atomic<bool>& raised, unsigned wgs, unsigned threads, unsigned lds, const FcI8& P, hipStream_t st) {
     if (lds > 64 * 1024 && !raised.load()) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
         if (e != hipSuccess) return e;
         raised.store(true);
     }
-    const size_t wgs = ((size_t)P.n_rows + MT * 16 - 1) / (MT * 16) * (((size_t)P.cout + NT * 16 - 1) / (NT * 16));
-    if (wgs > 0x7fffffffu) return hipErrorInvalidValue;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(WM * WN * 64), lds, st, P);
+    hipLaunchKernelGGL(kernel, dim3(wgs), dim3(threads), lds, st, P);
     return hipGetLastError();
 }
+template <typename T, int NB, int WAVES, int AHEAD, bool OWN>
+hipError_t rows_launch(const FcI8& P, hipStream_t st) {
+    static std::atomic<bool> raised{false};
+    const unsigned lds = 256 + (unsigned)std::max(OWN ? P.n_tiles * 64 : 0, WAVES * NB * 1024);
+    return launch_lds(fc_i8_rows_kernel<T, NB, WAVES, AHEAD, OWN>, raised, (unsigned)((P.cout + 15) / 16), WAVES * 64, lds, P, st);
+}
 template <typename T, int MT, int NT, int WM, int WN, int STAGES>
-hipError_t gemm(const FcI8& P, bool w_tiled, hipStream_t st) {
-    return w_tiled ? gemm_launch<T, MT, NT, WM, WN, STAGES, true>(P, st) : gemm_launch<T, MT, NT, WM, WN, STAGES, false>(P, st);
+hipError_t gemm(const FcI8& P, hipStream_t st) {
+    static std::atomic<bool> raised{false};
+    const size_t wgs = ((size_t)P.n_rows + MT * 16 - 1) / (MT * 16) * (((size_t)P.cout + NT * 16 - 1) / (NT * 16));
+    if (wgs > 0x7fffffffu) return hipErrorInvalidValue;
+    return launch_lds(fc_i8_gemm_kernel<T, MT, NT, WM, WN, STAGES>, raised, (unsigned)wgs, WM * WN * 64, STAGES * (MT + NT) * 2048, P, st);
 }
 
-// [cout][K] -> tiles, K padded with zeros, the last tile's missing rows left out
-__global__ __launch_bounds__(256) void tile_weights_kernel(const int8_t* __restrict__ w, int8_t* __restrict__ tiles, int K, int n_tiles, int cout) {
-    const int piece = (blockIdx.x * 256 + threadIdx.x) >> 4, r = blockIdx.y * 16 + (threadIdx.x & 15);
-    if (piece >= n_tiles * 4 || r >= cout) return;
-    *reinterpret_cast<intx4*>(tiles + tile_offset(r, piece * 16, n_tiles)) = weights16(w + (size_t)r * K, piece * 16, K);
+// [cout][K] -> rows of whole vectors, zeros behind K
+__global__ __launch_bounds__(256) void pad_weights_kernel(const int8_t* __restrict__ w, int8_t* __restrict__ to, int K, int width) {
+    const int k0 = (blockIdx.x * 256 + threadIdx.x) * 16;
+    if (k0 < width) *reinterpret_cast<intx4*>(to + (size_t)blockIdx.y * width + k0) = weights16(w + (size_t)blockIdx.y * K, k0, K);
 }
 
 template <typename T>
-hipError_t product(const FcI8& P, int8_t* w_tiles, hipStream_t st) {
-    const dim3 block(kI8Waves * 64);
-    const unsigned gx = (unsigned)((P.cout + 15) / 16);
-    if (P.n_rows <= 16)
-        hipLaunchKernelGGL((fc_i8_rows_kernel<T, 1>), dim3(gx, 1), block, 0, st, P);
-    else if (P.n_rows <= kI8FewRows)
-        hipLaunchKernelGGL((fc_i8_rows_kernel<T, 4>), dim3(gx, 1), block, 0, st, P);
-    else {
-        FcI8 Q = P;
-        if (w_tiles) {
-            hipLaunchKernelGGL(tile_weights_kernel, dim3((unsigned)((P.n_tiles * 4 + 15) / 16), gx), dim3(256), 0, st, P.w, w_tiles, P.K, P.n_tiles, P.cout);
-            const hipError_t e = hipGetLastError();
-            if (e != hipSuccess) return e;
-            Q.w = w_tiles;
-        }
-        const long big = ((long)P.n_rows + 255) / 256 * ((P.cout + 255) / 256), mid = ((long)P.n_rows + 127) / 128 * ((P.cout + 127) / 128);
-        if (big >= 192) return gemm<T, 16, 16, 2, 4, 4>(Q, w_tiles != nullptr, st);
-        if (mid >= 192) return gemm<T, 8, 8, 2, 2, 4>(Q, w_tiles != nullptr, st);
-        return gemm<T, 4, 4, 2, 2, 4>(Q, w_tiles != nullptr, st);
-    }
-    return hipGetLastError();
+hipError_t product_few(const FcI8& P, hipStream_t st) {
+    if (P.n_rows <= 16) return rows_launch<T, 1, 16, 2, false>(P, st);
+    if (P.n_rows <= 32) return rows_launch<T, 2, 8, 2, false>(P, st);
+    if (P.n_rows <= 48) return rows_launch<T, 3, 8, 2, false>(P, st);
+    return rows_launch<T, 4, 8, 2, false>(P, st);
+}
+template <typename T>
+hipError_t product_many(const FcI8& P, hipStream_t st) {
+    const long tiles = ((long)P.n_rows + 127) / 128 * ((P.cout + 127) / 128);
+    if (P.cout <= 64 && tiles > 64) return gemm<T, 8, 4, 2, 4, 2>(P, st);
+    if (tiles > 256) return gemm<T, 8, 8, 2, 4, 2>(P, st);
+    if (tiles > 128) return gemm<T, 8, 8, 2, 4, 3>(P, st);
+    return gemm<T, 4, 4, 2, 4, 4>(P, st);
 }
 
 }  // namespace
 
 hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, int8_t* q, float* scales, hipStream_t st) {
-    return dtype == DC_BF16 ? quantize<__hip_bfloat16, false>((const __hip_bfloat16*)x, n_rows, K, q, scales, st)
-                            : quantize<float, false>((const float*)x, n_rows, K, q, scales, st);
+    const Rows8 to{q, (size_t)K, K};
+    return dtype == DC_BF16 ? quantize<__hip_bfloat16, false>((const __hip_bfloat16*)x, n_rows, K, to, scales, st)
+                            : quantize<float, false>((const float*)x, n_rows, K, to, scales, st);
 }
 
-// The workspace: the rows in tiles, their scales, the weights in tiles.
-struct I8Space { size_t rows, scales, weights, end; };
+// The workspace: the rows in 8 bits, K padded with zeros to whole steps, their scales, and room for weights whose rows are not
+// whole vectors.
+struct I8Space { size_t scales, weights, end; };
 static I8Space i8_space(int n_rows, int K, int cout) {
-    const size_t row = ((size_t)K + 63) / 64 * 64;
+    if (n_rows == 1) return I8Space{0, 0, 0};
+    const size_t row = align_up(K, 128);
     I8Space s;
-    s.rows = 0;
     s.scales = align_up(align_up(n_rows, 16) * row, 256);
     s.weights = s.scales + align_up((size_t)n_rows * sizeof(float), 256);
-    s.end = s.weights + (n_rows > kI8FewRows ? align_up(align_up(cout, 16) * row, 256) : 0);
+    s.end = s.weights + (n_rows > kI8FewRows ? align_up(cout * row, 256) : 0);
     return s;
 }
 size_t fc_i8_workspace(int n_rows, int K, int cout) { return i8_space(n_rows, K, cout).end; }
 
+template <typename T>
+static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
+    const I8Space space = i8_space(P.n_rows, P.K, P.cout);
+    float* const sx = reinterpret_cast<float*>(ws + space.scales);
+    const int width = (int)align_up(P.K, 128);
+    P.x = x; P.n_tiles = width / 64; P.w_stride = P.K;
+    if (P.n_rows == 1) return rows_launch<T, 1, 16, 2, true>(P, st);
+    const bool few = P.n_rows <= kI8FewRows;
+    const Rows8 to{ws, (size_t)width, width};
+    P.xq = ws; P.x_stride = width; P.sx = sx;
+    hipError_t e = few ? quantize<T, true>(x, P.n_rows, P.K, to, sx, st) : quantize<T, false>(x, P.n_rows, P.K, to, sx, st);
+    if (e != hipSuccess) return e;
+    if (few) return product_few<T>(P, st);
+    if (P.K % 16 || reinterpret_cast<uintptr_t>(P.w) % 16) {
+        int8_t* const w = ws + space.weights;
+        for (int c = 0; c < P.cout; c += 65535) {
+            const int n = std::min(65535, P.cout - c);
+            hipLaunchKernelGGL(pad_weights_kernel, dim3((unsigned)((width / 16 + 255) / 256), (unsigned)n), dim3(256), 0, st, P.w + (size_t)c * P.K,
+                               w + (size_t)c * width, P.K, width);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        P.w = w; P.w_stride = width;
+    }
+    return product_many<T>(P, st);
+}
+
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
                         int dtype, void* ws, hipStream_t st) {
     FcI8 P;
-    P.n_rows = n_rows; P.K = K; P.n_tiles = (K + 63) / 64; P.cout = cout; P.relu = relu;
-    const I8Space space = i8_space(n_rows, K, cout);
-    int8_t* const base = static_cast<int8_t*>(ws);
-    float* const sx = reinterpret_cast<float*>(base + space.scales);
-    P.xq = base; P.sx = sx; P.w = w; P.sw = sw; P.bias = bias; P.out = out;
-    const hipError_t e = dtype == DC_BF16 ? quantize<__hip_bfloat16, true>((const __hip_bfloat16*)x, n_rows, K, base, sx, st)
-                                          : quantize<float, true>((const float*)x, n_rows, K, base, sx, st);
-    if (e != hipSuccess) return e;
-    const bool whole = K % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0;
-    int8_t* const w_tiles = whole ? nullptr : base + space.weights;
-    return dtype == DC_BF16 ? product<__hip_bfloat16>(P, w_tiles, st) : product<float>(P, w_tiles, st);
+    P.w = w; P.sw = sw; P.bias = bias; P.out = out;
+    P.n_rows = n_rows; P.K = K; P.cout = cout; P.relu = relu;
+    return dtype == DC_BF16 ? run_fc_i8((const __hip_bfloat16*)x, P, static_cast<int8_t*>(ws), st) : run_fc_i8((const float*)x, P, static_cast<int8_t*>(ws), st);
 }
 
 }  // namespace dc

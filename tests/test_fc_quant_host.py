@@ -7,7 +7,7 @@ import torch
 from paper_1712_01670_amd import binding
 
 
-def _layer(x=16, w=16, s=16, b=None, out=32, n=4, k=100, cout=8, relu=0, dtype=0, ws=256, nbytes=1 << 30):
+def _layer(x=16, w=16, s=16, b=None, out=32, n=40, k=100, cout=8, relu=0, dtype=0, ws=256, nbytes=1 << 30):
     p = lambda v: None if v is None else C.c_void_p(v)       # never dereferenced: validation fails first
     return binding.lib().dc_fc_quant_layer(p(x), p(w), p(s), p(b), p(out), n, k, cout, relu, dtype, p(ws), nbytes, None)
 
@@ -22,7 +22,7 @@ def test_refusals_of_the_layer():
     assert _layer(out=16) == -1                              # in place
     assert _layer(ws=264) == -1                              # a workspace that is not aligned
     need = C.c_size_t()
-    assert binding.lib().dc_fc_quant_workspace_bytes(4, 100, 8, C.byref(need)) == 0
+    assert binding.lib().dc_fc_quant_workspace_bytes(40, 100, 8, C.byref(need)) == 0 and need.value >= 40 * 100
     assert _layer(nbytes=need.value - 1) == -5
 
 
