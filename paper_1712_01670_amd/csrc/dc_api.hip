@@ -708,7 +708,7 @@ int32_t dc_moe_workspace_bytes(const dc_moe* moe, int32_t n_tokens, size_t* byte
     if (m.renormalize != 0 && m.renormalize != 1) return DC_ERR_INVALID_ARG;
     if (m.wtype != DC_F32 && m.wtype != DC_BF16 && m.wtype != DC_I8) return DC_ERR_INVALID_ARG;
     if (m.experts > kMoeMaxExperts || m.top_k > kMoeMaxTopK || n_tokens > kMoeMaxTokens) return DC_ERR_UNSUPPORTED;
-    if (m.cin > (1 << 24) || m.hidden > (1 << 24) || m.cout > (1 << 24)) return DC_ERR_UNSUPPORTED;
+    if (m.cin > (1 << 20) || m.hidden > (1 << 20) || m.cout > (1 << 20)) return DC_ERR_UNSUPPORTED;      // (offsets of a row in 32 bits)
     *bytes = moe_workspace(m, n_tokens);
     return DC_OK;
 }

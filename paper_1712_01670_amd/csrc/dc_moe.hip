@@ -26,28 +26,48 @@ struct Moe {
     void* out;                         // [n_tokens][cout]
     int32_t* choice;                   // [n_tokens][top_k]: an expert, or -1
     float* gate;                       // [n_tokens][top_k]
-    unsigned char* hidden_out;         // [n_tokens * top_k]: the experts' hidden values (hidden_row)
+    unsigned char* hidden_out;         // the experts' hidden values, in blocks of 16 slots (Chosen)
     int n_tokens, experts, top_k, cin, hidden, cout, renormalize;
-    int hidden_pad, cout_pad;          // hidden rounded up to 16, zeros behind it; cout rounded up to 4
+    int group_blocks, cout_pad;        // blocks of a group of tokens; cout rounded up to 4
     float* slot_out;                   // [n_tokens * top_k][cout_pad]: the experts' outputs
 };
 
 constexpr int kMoeTokens = 64;         // tokens that share one pass over the weights
-constexpr int kMoeWaves = 8;
+constexpr int kMoeWaves = 4;
 
-// N elements of a row from k0 on, at any address the type allows; zeros behind the row's end.
-template <typename E, int N>
-struct Piece { E v[N]; };
-template <int N, typename E>
-__device__ __forceinline__ Piece<E, N> piece(const E* __restrict__ row, int k0, int K) {
-    Piece<E, N> p;
-    if (k0 + N <= K) {
-        __builtin_memcpy(&p, row + k0, sizeof p);
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) p.v[e] = k0 + e < K ? row[k0 + e] : E{};
+// 16 bytes of a row, at any address the type allows.
+template <typename E>
+__device__ __forceinline__ uintx4 load16(const E* p) {
+    uintx4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+// The same from element k0 of a row of K, zeros behind its end: what overlaps the end comes from the row's last 16 bytes.
+template <typename E>
+__device__ __forceinline__ uintx4 load16_end(const E* __restrict__ row, int k0, int K) {
+    constexpr int N = 16 / sizeof(E);
+    if (k0 + N <= K) return load16(row + k0);
+    unsigned long long lo = 0, hi = 0;
+    if (k0 < K) {
+        if (K >= N) {
+            const uintx4 v = load16(row + K - N);
+            const int bits = (k0 - (K - N)) * (int)sizeof(E) * 8;      // 8 .. 120
+            lo = (unsigned long long)v[1] << 32 | v[0];
+            hi = (unsigned long long)v[3] << 32 | v[2];
+            if (bits >= 64) { lo = hi >> (bits - 64); hi = 0; }
+            else { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+        } else {
+#pragma unroll 1
+            for (int e = 0; k0 + e < K; ++e) {
+                typename std::conditional<sizeof(E) == 4, uint32_t, typename std::conditional<sizeof(E) == 2, uint16_t, uint8_t>::type>::type u;
+                __builtin_memcpy(&u, row + k0 + e, sizeof u);
+                const int bit = e * (int)sizeof(E) * 8;
+                if (bit < 64) lo |= (unsigned long long)u << bit;
+                else hi |= (unsigned long long)u << (bit - 64);
+            }
+        }
     }
-    return p;
+    return uintx4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
 
 // A wavefront's operand for 4 * PE values of K, PE of them a lane (16 bytes of weights): one or more fragments of the matrix
@@ -57,10 +77,9 @@ struct Operand {
     static constexpr int PE = 16 / sizeof(W), V = PE * sizeof(T) / 16;     // V: 16-byte vectors
     uintx4 v[V];
     // of the tokens' own type
-    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(v, p, sizeof v); }
-    __device__ __forceinline__ void load(const T* row, int k0, int K) {
-        const Piece<T, PE> t = piece<PE>(row, k0, K);
-        __builtin_memcpy(v, &t, sizeof v);
+    __device__ __forceinline__ void load_end(const T* row, int k0, int K) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = load16_end(row, k0 + i * (16 / (int)sizeof(T)), K);
     }
     // from weights as they lie in memory
     __device__ __forceinline__ explicit Operand(const uintx4& w) {
@@ -111,36 +130,48 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A workgroup takes a token: its wavefronts deal the experts among themselves, four at a time, the first one chooses.
-constexpr int kRouterWaves = 8;
+// A workgroup takes a token: its wavefronts deal the experts among themselves, the first one chooses.
+constexpr int kRouterWaves = 16;
 template <typename T>
 __global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
-    constexpr int VE = 16 / sizeof(T), EB = 4;
+    constexpr int VE = 16 / sizeof(T), AT_ONCE = 4;
     __shared__ float logits[kMoeMaxExperts];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x;
     const T* const x = static_cast<const T*>(P.x) + (size_t)token * P.cin;
-    const T* const router = static_cast<const T*>(P.router);
-    for (int e0 = wave * EB; e0 < P.experts; e0 += kRouterWaves * EB) {
-        float sum[EB] = {};
-        const T* w[EB];
+    for (int e = wave; e < P.experts; e += kRouterWaves) {
+        const T* const w = static_cast<const T*>(P.router) + (size_t)e * P.cin;
+        const float bias = P.router_bias ? P.router_bias[e] : 0.f;
+        float sum = 0.f;
+        for (int k0 = lane * VE; k0 < P.cin; k0 += AT_ONCE * 64 * VE) {
+            uintx4 xv[AT_ONCE], wv[AT_ONCE];
+            if (k0 - lane * VE + AT_ONCE * 64 * VE <= P.cin) {
 #pragma unroll
-        for (int i = 0; i < EB; ++i) w[i] = router + (size_t)min(e0 + i, P.experts - 1) * P.cin;
-#pragma unroll 2
-        for (int k = lane * VE; k < P.cin; k += 64 * VE) {
-            const Piece<T, VE> xv = piece<VE>(x, k, P.cin);
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    xv[i] = load16(x + k0 + i * 64 * VE);
+                    wv[i] = load16(w + k0 + i * 64 * VE);
+                }
+            } else {
 #pragma unroll
-            for (int i = 0; i < EB; ++i) {
-                const Piece<T, VE> wv = piece<VE>(w[i], k, P.cin);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) sum[i] = fmaf(to_float(xv.v[e]), to_float(wv.v[e]), sum[i]);
+                for (int i = 0; i < AT_ONCE; ++i) {
+                    xv[i] = load16_end(x, k0 + i * 64 * VE, P.cin);
+                    wv[i] = load16_end(w, k0 + i * 64 * VE, P.cin);
+                }
             }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    if constexpr (sizeof(T) == 4) {
+                        sum = fmaf(__uint_as_float(xv[i][d]), __uint_as_float(wv[i][d]), sum);
+                    } else {
+                        sum = fmaf(__uint_as_float(xv[i][d] << 16), __uint_as_float(wv[i][d] << 16), sum);
+                        sum = fmaf(__uint_as_float(xv[i][d] & 0xffff0000u), __uint_as_float(wv[i][d] & 0xffff0000u), sum);
+                    }
+                }
         }
 #pragma unroll
-        for (int i = 0; i < EB; ++i) {
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) sum[i] += __shfl_xor(sum[i], d);
-            if (lane == i && e0 + i < P.experts) logits[e0 + i] = sum[i] + (P.router_bias ? P.router_bias[e0 + i] : 0.f);
-        }
+        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) logits[e] = sum + bias;
     }
     __syncthreads();
     if (wave != 0) return;
@@ -192,116 +223,154 @@ __global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
 }
 
 // ---- the experts ----------------------------------------------------------------------------------------------------------
-// The slots (token * top_k + choice) of a group of kMoeTokens tokens, by expert: which experts have any, and their slots in
-// order.  Made by every workgroup for itself.
+// The slots (token * top_k + choice) of a group of kMoeTokens tokens, by expert.  Every workgroup finds its own: the choices are a few
+// hundred numbers.  An expert's slots are dealt in parts of 32, a workgroup each; the hidden values of its i-th slot stand in
+// row i % 16 of block base + i / 16, base being the blocks of the experts before.
+constexpr int kMoePart = 32;
 struct Chosen {
-    uint32_t has[kMoeMaxExperts / 32];
-    int slot[kMoeTokens];              // of one expert
-    int n;
+    int count[kMoeMaxExperts];             // slots of an expert
+    int choice[kMoeTokens * kMoeMaxTopK];
+    int slot[kMoePart];                    // of this workgroup's part
 };
-__device__ __forceinline__ void find_experts(const Moe& P, Chosen& C, int t0, int n_tok) {
-    for (int i = threadIdx.x; i < kMoeMaxExperts / 32; i += blockDim.x) C.has[i] = 0;
+__device__ __forceinline__ void count_experts(const Moe& P, Chosen& C, int t0, int n_tok) {
+    constexpr int THREADS = kMoeWaves * 64, N = kMoeTokens * kMoeMaxTopK / THREADS;
+    const int n = n_tok * P.top_k, tid = threadIdx.x;
+    int mine[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) mine[i] = tid + i * THREADS < n ? P.choice[(size_t)t0 * P.top_k + tid + i * THREADS] : -1;
+    for (int i = tid; i < kMoeMaxExperts; i += THREADS) C.count[i] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n_tok * P.top_k; i += blockDim.x) {
-        const int e = P.choice[(size_t)t0 * P.top_k + i];
-        if (e >= 0) atomicOr(&C.has[e >> 5], 1u << (e & 31));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int at = tid + i * THREADS;
+        if (at < n) C.choice[at] = mine[i];
+        if (mine[i] >= 0) atomicAdd(&C.count[mine[i]], 1);
     }
     __syncthreads();
 }
-// The a-th expert that has tokens, or -1.
-__device__ __forceinline__ int nth_expert(const Chosen& C, int a) {
-    for (int i = 0; i < kMoeMaxExperts / 32; ++i) {
-        uint32_t m = C.has[i];
-        const int c = __popc(m);
-        if (a >= c) { a -= c; continue; }
-        for (; a > 0; --a) m &= m - 1;
-        return i * 32 + __ffs((int)m) - 1;
+// The a-th part: its expert (-1: there are fewer), its place among the expert's parts, the expert's slots and first block.  Every
+// wavefront for itself: a lane per expert, sums over the lanes before.
+struct Part { int e, place, n, block; };
+__device__ __forceinline__ Part find_part(const Moe& P, const Chosen& C, int a) {
+    const int lane = threadIdx.x & 63;
+    Part part{-1, 0, 0, 0};
+    int parts = 0, blocks = 0;                 // of the experts before
+    for (int i = 0; i * 64 < P.experts && part.e < 0; ++i) {
+        const int n = C.count[i * 64 + lane], own = (n + kMoePart - 1) / kMoePart << 16 | (n + 15) / 16;
+        int sum = own;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        const int before = parts + ((sum - own) >> 16);
+        const unsigned long long hit = __ballot(a >= before && a < before + (own >> 16));
+        if (hit) {
+            const int l = __ffsll(hit) - 1;
+            part.e = i * 64 + l;
+            part.place = a - __builtin_amdgcn_readlane(before, l);
+            part.n = __builtin_amdgcn_readlane(n, l);
+            part.block = blocks + __builtin_amdgcn_readlane((sum - own) & 0xffff, l);
+        }
+        const int all = __builtin_amdgcn_readlane(sum, 63);
+        parts += all >> 16;
+        blocks += all & 0xffff;
     }
-    return -1;
+    return part;
 }
-// Slots of expert e, by the first wavefront: a lane per token.
-__device__ __forceinline__ void list_slots(const Moe& P, Chosen& C, int e, int t0, int n_tok) {
+// Slots of the part in order, by the first wavefront, a lane per token.
+__device__ __forceinline__ void list_slots(const Moe& P, Chosen& C, const Part& part, int t0, int n_tok) {
     if (threadIdx.x < 64) {
         int at = -1;
         if ((int)threadIdx.x < n_tok)
             for (int j = 0; j < P.top_k; ++j)
-                if (P.choice[(size_t)(t0 + threadIdx.x) * P.top_k + j] == e) at = (t0 + threadIdx.x) * P.top_k + j;
+                if (C.choice[threadIdx.x * P.top_k + j] == part.e) at = (t0 + threadIdx.x) * P.top_k + j;
         const unsigned long long m = __ballot(at >= 0);
-        if (at >= 0) C.slot[__popcll(m & ((1ull << threadIdx.x) - 1))] = at;
-        if (threadIdx.x == 0) C.n = __popcll(m);
+        const int i = __popcll(m & ((1ull << threadIdx.x) - 1)) - part.place * kMoePart;
+        if (at >= 0 && i >= 0 && i < kMoePart) C.slot[i] = at;
     }
     __syncthreads();
 }
 
-// Hidden values of a slot: fp32, or two bf16 numbers each (the value's rounding and what that leaves) in two rows, so that the
-// second product sees 16 bits of them: the layer's output is rounded once, as if they were fp32.
-template <typename T>
-__device__ __forceinline__ T* hidden_row(const Moe& P, int slot) {
-    return reinterpret_cast<T*>(P.hidden_out) + (size_t)slot * P.hidden_pad * (sizeof(T) == 2 ? 2 : 1);
+// The product of R tiles of 16 channels of an expert (gated: R / 2 in either half) with a part of its slots: relu or gate of
+// the first layer into the hidden values, or the second layer into the slots' outputs.  The weights are what has to come from
+// memory, once: they go straight into operands (16 rows of 64 bytes an instruction), three pieces of a wavefront
+// ahead, and K is dealt among the wavefronts by pairs of pieces, whole cache lines; their sums are added through LDS in a fixed
+// order.  The tokens' rows come from L2, a piece ahead, once for R tiles of weights: a row of a fragment costs the CU a look-up for
+// every 16 bytes, as a row of weights does, so R is large where there are workgroups enough.  The hidden values lie in the order
+// of the second layer's fragments, 1 KiB a look-up of 16, fp32 or as two bf16 numbers each (the value's rounding and what
+// that leaves), so that the second product sees 16 bits of them: the layer's output is rounded once, as if they were fp32.
+__device__ __forceinline__ int opaque(int v) {      // a value the optimiser computes nothing from ahead of time
+    asm volatile("" : "+v"(v));
+    return v;
 }
-
-// The product of 32 channels of an expert (gated: of 16 in either half) with all its tokens of a group: relu or gate of the first
-// layer into the hidden values, or the second layer into the slots' outputs.  The weights are what has to come from memory, once:
-// they go straight into operands (16 rows of 64 bytes an instruction), three pieces of a wavefront ahead, and K is dealt among the
-// wavefronts by pairs of pieces, whole cache lines; their sums are added through LDS in a fixed order.  The tokens' rows come from
-// L2, a piece ahead, once for both tiles of weights.
 enum { kUpRelu = 0, kUpGated = 1, kDown = 2 };
-template <typename T, typename W, int KIND, int MOST>
+template <typename T, typename W, int KIND, int R, int MOST>
 __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     typedef Operand<T, W> Op;
-    constexpr int PE = Op::PE, HALVES = KIND == kUpGated ? 2 : 1, R = 2, CT = R / HALVES;
-    constexpr bool DOWN = KIND == kDown, TWO = DOWN && sizeof(T) == 2;      // TWO: a row is two
+    constexpr int PE = Op::PE, V = Op::V, HALVES = KIND == kUpGated ? 2 : 1, CT = R / HALVES, PLANES = sizeof(T) == 2 ? 2 : 1;
+    constexpr bool DOWN = KIND == kDown, TWO = DOWN && PLANES == 2;
     __shared__ Chosen C;
     __shared__ floatx4 red[kMoeWaves][R][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
-    const int channels = DOWN ? P.cout : P.hidden, K = DOWN ? P.hidden : P.cin, row_end = DOWN ? P.hidden_pad : P.cin;
+    const int channels = DOWN ? P.cout : P.hidden, K = DOWN ? P.hidden : P.cin;
     const int o0 = blockIdx.x * (CT * 16), t0 = blockIdx.z * kMoeTokens, n_tok = min(kMoeTokens, P.n_tokens - t0);
-    find_experts(P, C, t0, n_tok);
-    const int e = nth_expert(C, blockIdx.y);
+    const int pieces = (K + 4 * PE - 1) / (4 * PE), whole = K / (4 * PE), hidden_pieces = (P.hidden + 4 * PE - 1) / (4 * PE);
+    count_experts(P, C, t0, n_tok);
+    const Part part = find_part(P, C, blockIdx.y);
+    const int e = part.e;
     if (e < 0) return;
-    list_slots(P, C, e, t0, n_tok);
-    const int n = C.n, pieces = (K + 4 * PE - 1) / (4 * PE), whole = K / (4 * PE);
-    const W* wrow[R];                      // tile r: half r / CT, channels 16 (r % CT) on; past the end the last channel again
+    // Addresses are a uniform base and 32 bits a lane, so that what is ahead costs no registers but its own.  Tile r: half r / CT,
+    // channels 16 (r % CT) on; past the end the last channel again.
+    const unsigned char* wbase[HALVES];
+    uint32_t wat[CT];
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-        wrow[r] = static_cast<const W*>(DOWN ? P.down : P.up) + (((size_t)e * HALVES + r / CT) * channels + min(o0 + r % CT * 16 + l16, channels - 1)) * K + g * PE;
-    auto product = [&](auto blocks) {
+    for (int h = 0; h < HALVES; ++h)
+        wbase[h] = reinterpret_cast<const unsigned char*>(static_cast<const W*>(DOWN ? P.down : P.up) + (((size_t)e * HALVES + h) * channels + o0) * K);
+#pragma unroll
+    for (int c = 0; c < CT; ++c) wat[c] = (uint32_t)max(0, min(c * 16 + l16, channels - 1 - o0)) * (uint32_t)(K * sizeof(W)) + g * 16;
+    auto at = [&](int i) { return (wave + i / 2 * kMoeWaves) * 2 + i % 2; };       // piece i of this wavefront
+    uintx4 w[4][R];
+    auto fetch_w = [&](uintx4 (&to)[R], int p) {
+        if (p < whole)
+#pragma unroll
+            for (int r = 0; r < R; ++r) to[r] = load16(wbase[r / CT] + (uint32_t)(p * 64) + wat[r % CT]);
+    };
+#pragma unroll
+    for (int d = 0; d < 3; ++d) fetch_w(w[d], at(d));
+    list_slots(P, C, part, t0, n_tok);                     // (while the first weights travel)
+    const int n = min(kMoePart, part.n - part.place * kMoePart);
+    unsigned char* const tiles = P.hidden_out + ((size_t)blockIdx.z * P.group_blocks + part.block + part.place * (kMoePart / 16)) * PLANES * hidden_pieces * (V * 1024);
+    auto product = [&](auto blocks) {                      // of 16 slots
         constexpr int NB = decltype(blocks)::value;
-        const T* xrow[NB];
+        const unsigned char* xbase[DOWN ? NB : 1];
+        uint32_t xat[DOWN ? 1 : NB];
+        if constexpr (DOWN) {
+            xat[0] = lane * 16;
 #pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const int slot = C.slot[min(j * 16 + l16, n - 1)];
-            xrow[j] = (DOWN ? hidden_row<T>(P, slot) : static_cast<const T*>(P.x) + (size_t)(slot / P.top_k) * P.cin) + g * PE;
+            for (int j = 0; j < NB; ++j) xbase[j] = tiles + (size_t)j * PLANES * hidden_pieces * (V * 1024);
+        } else {
+            xbase[0] = static_cast<const unsigned char*>(P.x);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) xat[j] = (uint32_t)(C.slot[min(j * 16 + l16, n - 1)] / P.top_k) * (uint32_t)(P.cin * sizeof(T));
         }
-        // piece i of this wavefront
-        auto at = [&](int i) { return (wave + i / 2 * kMoeWaves) * 2 + i % 2; };
-        uintx4 w[4][R];
         Op x[2][NB], low[2][TWO ? NB : 1];
-        auto fetch_w = [&](uintx4 (&to)[R], int p) {
-            if (p < whole) {
+        auto fetch_x = [&](int b, int p, bool end = false, int k0 = 0) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) __builtin_memcpy(&to[r], wrow[r] + p * (4 * PE), 16);
-            } else if (p < pieces) {
+            for (int j = 0; j < NB; ++j) {
+                if constexpr (DOWN) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const Piece<W, PE> t = piece<PE>(wrow[r], p * (4 * PE), K - g * PE);
-                    __builtin_memcpy(&to[r], &t, 16);
-                }
-            }
-        };
-        auto fetch_x = [&](int b, int p) {
-            if (p < whole) {
+                    for (int v = 0; v < V; ++v) {
+                        const unsigned char* const from = xbase[j] + (uint32_t)((p * V + v) * 1024);
+                        x[b][j].v[v] = load16(from + xat[0]);
+                        if constexpr (TWO) low[b][j].v[v] = load16(from + (uint32_t)(hidden_pieces * (V * 1024)) + xat[0]);
+                    }
+                } else if (end) {
+                    x[b][j].load_end(reinterpret_cast<const T*>(xbase[0] + xat[j]), k0, K);
+                } else {
 #pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    x[b][j].load(xrow[j] + p * (4 * PE));
-                    if constexpr (TWO) low[b][j].load(xrow[j] + P.hidden_pad + p * (4 * PE));
-                }
-            } else if (p < pieces) {
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    x[b][j].load(xrow[j], p * (4 * PE), row_end - g * PE);
-                    if constexpr (TWO) low[b][j].load(xrow[j] + P.hidden_pad, p * (4 * PE), row_end - g * PE);
+                    for (int v = 0; v < V; ++v) x[b][j].v[v] = load16(xbase[0] + (uint32_t)(p * (V * 64) + v * 16) + (xat[j] + g * (V * 16)));
                 }
             }
         };
@@ -310,39 +379,46 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int j = 0; j < NB; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-        fetch_w(w[0], at(0));
-        fetch_w(w[1], at(1));
-        fetch_x(0, at(0));
-        fetch_w(w[2], at(2));
-        for (int i = 0; at(i) < pieces; i += 4) {
+        auto multiply = [&](const uintx4 (&weights)[R], int b) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                uintx4 raw = weights[r];
+                asm volatile("" : "+v"(raw));                  // (converted here, not where it is loaded: the ring holds bytes)
+                const Op o(raw);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    mma(o, x[b][j], acc[r][j]);
+                    if constexpr (TWO) mma(o, low[b][j], acc[r][j]);
+                }
+            }
+        };
+        if (at(0) < whole) fetch_x(0, at(0));
+        for (int i = 0; at(i) < whole; i += 4) {
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                fetch_x((d + 1) & 1, at(i + d + 1));           // (loads come back in order: the rows before the weights further ahead)
-                fetch_w(w[(d + 3) & 3], at(i + d + 3));
+                if (at(i + d + 1) < whole) fetch_x((d + 1) & 1, at(i + d + 1));      // (loads come back in order: the rows before the
+                fetch_w(w[(d + 3) & 3], at(i + d + 3));                                     // weights further ahead)
                 __builtin_amdgcn_sched_barrier(0);
-                if (at(i + d) < pieces) {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        const Op o(w[d][r]);
-#pragma unroll
-                        for (int j = 0; j < NB; ++j) {
-                            mma(o, x[d & 1][j], acc[r][j]);
-                            if constexpr (TWO) mma(o, low[d & 1][j], acc[r][j]);
-                        }
-                    }
-                }
+                if (at(i + d) < whole) multiply(w[d], d & 1);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
+        if (pieces > whole && wave == whole / 2 % kMoeWaves) {         // the piece that K ends in
+            const int k0 = opaque(whole * (4 * PE) + g * PE);
+#pragma unroll
+            for (int r = 0; r < R; ++r) w[0][r] = load16_end(reinterpret_cast<const W*>(wbase[r / CT] + (wat[r % CT] - g * 16)), k0, K);
+            fetch_x(0, whole, true, k0);
+            multiply(w[0], 0);
+        }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            if (j) __syncthreads();
+            __syncthreads();
 #pragma unroll
             for (int r = 0; r < R; ++r) red[wave][r][lane] = acc[r][j];
             __syncthreads();
-            const int at = j * 16 + l16, ct = wave;            // wavefront ct: tile ct of the channels
-            if (ct >= CT || at >= n) continue;
-            const int slot = C.slot[at], c0 = o0 + ct * 16 + g * 4;
+            const int i = j * 16 + l16, ct = wave;      // wavefront ct: tile ct of the channels
+            if (ct >= CT || i >= n) continue;
+            const int slot = C.slot[i], c0 = opaque(o0 + ct * 16 + g * 4);       // (what follows from it is not worth registers in the loop)
             floatx4 sum[HALVES];
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
@@ -350,36 +426,39 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
 #pragma unroll
                 for (int v = 1; v < kMoeWaves; ++v) sum[h] += red[v][h * CT + ct][lane];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const size_t c = ((size_t)e * HALVES + h) * channels + min(c0 + i, channels - 1);
+                for (int q = 0; q < 4; ++q) {
+                    const size_t c = ((size_t)e * HALVES + h) * channels + min(c0 + q, channels - 1);
                     const float* const bias = DOWN ? P.down_bias : P.up_bias;
-                    sum[h][i] = sum[h][i] * (sizeof(W) == 1 ? (DOWN ? P.down_scale : P.up_scale)[c] : 1.f) + (bias ? bias[c] : 0.f);
+                    sum[h][q] = sum[h][q] * (sizeof(W) == 1 ? (DOWN ? P.down_scale : P.up_scale)[c] : 1.f) + (bias ? bias[c] : 0.f);
                 }
             }
             if constexpr (DOWN) {
                 if (c0 < P.cout_pad) *reinterpret_cast<floatx4*>(P.slot_out + (size_t)slot * P.cout_pad + c0) = sum[0];
             } else {
-                T* const out = hidden_row<T>(P, slot) + c0;
+                if (c0 >= hidden_pieces * 4 * PE) continue;
+                T high[4], rest[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float u = sum[0][i];
+                for (int q = 0; q < 4; ++q) {
+                    const float u = sum[0][q];
                     float v;
-                    if constexpr (KIND == kUpGated) v = u / (1.f + expf(-u)) * sum[HALVES - 1][i];
+                    if constexpr (KIND == kUpGated) v = u / (1.f + expf(-u)) * sum[HALVES - 1][q];
                     else v = u > 0.f || u != u ? u : 0.f;
-                    if (c0 + i >= P.hidden) v = 0.f;
-                    if (c0 + i >= P.hidden_pad) continue;
-                    store(out + i, v);
-                    if constexpr (sizeof(T) == 2) {
-                        const float high = to_float(to_bf16(v));
-                        store(out + P.hidden_pad + i, fabsf(high) < INFINITY || high != high ? v - high : 0.f);
-                    }
+                    if (c0 + q >= P.hidden) v = 0.f;           // behind the last channel the second layer multiplies zeros
+                    store(&high[q], v);
+                    const float h = to_float(high[q]);
+                    store(&rest[q], fabsf(h) < INFINITY || h != h ? v - h : 0.f);
                 }
+                // channel c0 is element c0 % PE of lane group c0 / PE % 4 of piece c0 / (4 PE)
+                constexpr int VE = 16 / sizeof(T);
+                unsigned char* const to = tiles + (size_t)j * PLANES * hidden_pieces * (V * 1024) +
+                                          ((size_t)(c0 / (4 * PE)) * V + c0 % PE / VE) * 1024 + (c0 / PE % 4 * 16 + l16) * 16 + c0 % VE * sizeof(T);
+                __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(T)), high, sizeof high);
+                if constexpr (PLANES == 2) __builtin_memcpy(__builtin_assume_aligned(to + (size_t)hidden_pieces * (V * 1024), 4 * sizeof(T)), rest, sizeof rest);
             }
         }
     };
     if (MOST == 1 || n <= 16) product(std::integral_constant<int, 1>());
-    else if (n <= 32) product(std::integral_constant<int, 2>());
-    else product(std::integral_constant<int, 4>());
+    else product(std::integral_constant<int, 2>());
 }
 
 // out[token] = sum over its choices of gate * the slot's output
@@ -402,15 +481,25 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
         if (c + i < P.cout) store(out + i, sum[i]);
 }
 
+template <typename T, typename W, int KIND, int R>
+hipError_t expert_launch_as(const Moe& P, unsigned tiles, unsigned active, hipStream_t st) {
+    const dim3 grid(tiles, active, (unsigned)((P.n_tokens + kMoeTokens - 1) / kMoeTokens)), block(kMoeWaves * 64);
+    if (P.n_tokens <= 16) hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 1>), grid, block, 0, st, P);
+    else hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 2>), grid, block, 0, st, P);
+    return hipGetLastError();
+}
+// As many tiles of channels a workgroup as leave a workgroup for every CU.
 template <typename T, typename W, int KIND>
 hipError_t expert_launch(const Moe& P, hipStream_t st) {
-    const unsigned groups = (unsigned)((P.n_tokens + kMoeTokens - 1) / kMoeTokens);
-    const unsigned active = (unsigned)std::min(P.experts, std::min(P.n_tokens, kMoeTokens) * P.top_k);      // at most
-    const unsigned tiles = (unsigned)((KIND == kDown ? P.cout : P.hidden) + (KIND == kUpGated ? 15 : 31)) / (KIND == kUpGated ? 16 : 32);
-    const dim3 grid(tiles, active, groups), block(kMoeWaves * 64);
-    if (P.n_tokens <= 16) hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, 1>), grid, block, 0, st, P);
-    else hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, 4>), grid, block, 0, st, P);
-    return hipGetLastError();
+    const int slots = std::min(P.n_tokens, kMoeTokens) * P.top_k;
+    const unsigned active = (unsigned)(std::min(P.experts, slots) + (P.n_tokens > kMoePart ? slots / (kMoePart + 1) : 0));      // parts, at most
+    constexpr unsigned kHalves = KIND == kUpGated ? 2 : 1, kPiece = 64 / sizeof(W);
+    const unsigned channels = KIND == kDown ? (unsigned)P.cout : ((unsigned)P.hidden + kPiece - 1) / kPiece * kPiece;      // (whole pieces of hidden values)
+    auto tiles = [&](unsigned r) { return (channels + 16 * r / kHalves - 1) / (16 * r / kHalves); };
+    if (tiles(4) * active >= 256) return expert_launch_as<T, W, KIND, 4>(P, tiles(4), active, st);
+    if constexpr (kHalves == 1)
+        if (tiles(2) * active < 256) return expert_launch_as<T, W, KIND, 1>(P, tiles(1), active, st);
+    return expert_launch_as<T, W, KIND, 2>(P, tiles(2), active, st);
 }
 
 template <typename T, typename W>
@@ -428,12 +517,17 @@ hipError_t moe_run(const Moe& P, bool gated, hipStream_t st) {
 
 // The workspace: the choice (where the caller does not take it), the hidden values and the outputs of every slot.
 struct MoeSpace { size_t gate, hidden, slots, end; };
+static size_t group_blocks(const dc_moe& m, int n_tokens) {
+    const int tokens = std::min(n_tokens, kMoeTokens);
+    return ((size_t)tokens * m.top_k + 15 * (size_t)std::min(m.experts, tokens * m.top_k)) / 16;
+}
 static MoeSpace moe_space(const dc_moe& m, int n_tokens) {
     const size_t slots = (size_t)n_tokens * m.top_k;
     MoeSpace s;
     s.gate = align_up(slots * 4, 256);
     s.hidden = 2 * s.gate;
-    s.slots = s.hidden + align_up(slots * align_up(m.hidden, 16) * 4, 256);
+    // (rows of the type's own size or two of half of it; an expert's last block is not full)
+    s.slots = s.hidden + ((size_t)n_tokens + kMoeTokens - 1) / kMoeTokens * group_blocks(m, n_tokens) * 16 * align_up(m.hidden, 64) * 4;
     s.end = s.slots + align_up(slots * align_up(m.cout, 4) * 4, 256);
     return s;
 }
@@ -453,7 +547,7 @@ hipError_t launch_moe(const dc_moe& m, const dc_moe_weights& w, const void* in, 
     P.hidden_out = base + space.hidden;
     P.slot_out = reinterpret_cast<float*>(base + space.slots);
     P.n_tokens = n_tokens; P.experts = m.experts; P.top_k = m.top_k; P.cin = m.cin; P.hidden = m.hidden; P.cout = m.cout;
-    P.renormalize = m.renormalize; P.hidden_pad = (int)align_up(m.hidden, 16); P.cout_pad = (int)align_up(m.cout, 4);
+    P.renormalize = m.renormalize; P.group_blocks = (int)group_blocks(m, n_tokens); P.cout_pad = (int)align_up(m.cout, 4);
     const bool gated = m.act == DC_MOE_GATED;
     if (dtype == DC_BF16) return m.wtype == DC_I8 ? moe_run<uint16_t, int8_t>(P, gated, st) : moe_run<uint16_t, uint16_t>(P, gated, st);
     return m.wtype == DC_I8 ? moe_run<float, int8_t>(P, gated, st) : moe_run<float, float>(P, gated, st);
