@@ -1,7 +1,8 @@
 // A mixture-of-experts layer for a few tokens (a row per video stream): a router chooses top_k of the experts for every token,
 // an expert is a pair of fully-connected layers, and the token's output is the sum of its experts', weighted by the router's
-// softmax.  What bounds it is the weights of the chosen experts, each of which is read once for up to 64 tokens; four launches:
-// the choice, the experts' first layers, their second layers, the weighted sum.
+// softmax.  What bounds it is the weights of the chosen experts, each of which is read once for up to 32 of its tokens.  Launches:
+// the choice, the experts' first layers, their second layers, the weighted sum; up to 16 tokens the second layers' last workgroups add
+// up, and where the choice is quick every workgroup of the first layers makes it for itself: two launches are left.
 #include <hip/hip_bf16.h>
 
 #include <algorithm>
@@ -30,6 +31,8 @@ struct Moe {
     int n_tokens, experts, top_k, cin, hidden, cout, renormalize;
     int group_blocks, cout_pad;        // blocks of a group of tokens; cout rounded up to 4
     float* slot_out;                   // [n_tokens * top_k][cout_pad]: the experts' outputs
+    int32_t* done;                     // [down_tiles], up to 16 tokens: workgroups of the second layers that have written theirs
+    int down_tiles, route;             // route: the first layers' kernel makes the choice itself
 };
 
 constexpr int kMoeTokens = 64;         // tokens that share one pass over the weights
@@ -130,52 +133,63 @@ __device__ __forceinline__ uint32_t logit_key(float l) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A workgroup takes a token: its wavefronts deal the experts among themselves, the first one chooses.
-constexpr int kRouterWaves = 16;
-template <typename T>
-__global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
+// A wavefront's logits of N experts from e0 on, STEP apart, for a token: the same operations in the same order wherever it is called.
+template <typename T, int N, int STEP>
+__device__ __forceinline__ void router_logits(const Moe& P, int token, int e0, float* logits) {
     constexpr int VE = 16 / sizeof(T), AT_ONCE = 4;
-    __shared__ float logits[kMoeMaxExperts];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x;
+    const int lane = threadIdx.x & 63;
     const T* const x = static_cast<const T*>(P.x) + (size_t)token * P.cin;
-    for (int e = wave; e < P.experts; e += kRouterWaves) {
-        const T* const w = static_cast<const T*>(P.router) + (size_t)e * P.cin;
-        const float bias = P.router_bias ? P.router_bias[e] : 0.f;
-        float sum = 0.f;
-        for (int k0 = lane * VE; k0 < P.cin; k0 += AT_ONCE * 64 * VE) {
-            uintx4 xv[AT_ONCE], wv[AT_ONCE];
-            if (k0 - lane * VE + AT_ONCE * 64 * VE <= P.cin) {
+    const T* w[N];
+    float sum[N], bias[N];
 #pragma unroll
-                for (int i = 0; i < AT_ONCE; ++i) {
-                    xv[i] = load16(x + k0 + i * 64 * VE);
-                    wv[i] = load16(w + k0 + i * 64 * VE);
-                }
-            } else {
+    for (int i = 0; i < N; ++i) {
+        const int e = min(e0 + i * STEP, P.experts - 1);
+        w[i] = static_cast<const T*>(P.router) + (size_t)e * P.cin;
+        bias[i] = P.router_bias ? P.router_bias[e] : 0.f;
+        sum[i] = 0.f;
+    }
+    for (int k0 = lane * VE; k0 < P.cin; k0 += AT_ONCE * 64 * VE) {
+        uintx4 xv[AT_ONCE], wv[N][AT_ONCE];
+        if (k0 - lane * VE + AT_ONCE * 64 * VE <= P.cin) {
 #pragma unroll
-                for (int i = 0; i < AT_ONCE; ++i) {
-                    xv[i] = load16_end(x, k0 + i * 64 * VE, P.cin);
-                    wv[i] = load16_end(w, k0 + i * 64 * VE, P.cin);
-                }
+            for (int a = 0; a < AT_ONCE; ++a) {
+                xv[a] = load16(x + k0 + a * 64 * VE);
+#pragma unroll
+                for (int i = 0; i < N; ++i) wv[i][a] = load16(w[i] + k0 + a * 64 * VE);
             }
+        } else {
 #pragma unroll
-            for (int i = 0; i < AT_ONCE; ++i)
+            for (int a = 0; a < AT_ONCE; ++a) {
+                xv[a] = load16_end(x, k0 + a * 64 * VE, P.cin);
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    if constexpr (sizeof(T) == 4) {
-                        sum = fmaf(__uint_as_float(xv[i][d]), __uint_as_float(wv[i][d]), sum);
-                    } else {
-                        sum = fmaf(__uint_as_float(xv[i][d] << 16), __uint_as_float(wv[i][d] << 16), sum);
-                        sum = fmaf(__uint_as_float(xv[i][d] & 0xffff0000u), __uint_as_float(wv[i][d] & 0xffff0000u), sum);
-                    }
-                }
+                for (int i = 0; i < N; ++i) wv[i][a] = load16_end(w[i], k0 + a * 64 * VE, P.cin);
+            }
         }
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-        if (lane == 0) logits[e] = sum + bias;
+        for (int a = 0; a < AT_ONCE; ++a)
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    if constexpr (sizeof(T) == 4) {
+                        sum[i] = fmaf(__uint_as_float(xv[a][d]), __uint_as_float(wv[i][a][d]), sum[i]);
+                    } else {
+                        sum[i] = fmaf(__uint_as_float(xv[a][d] << 16), __uint_as_float(wv[i][a][d] << 16), sum[i]);
+                        sum[i] = fmaf(__uint_as_float(xv[a][d] & 0xffff0000u), __uint_as_float(wv[i][a][d] & 0xffff0000u), sum[i]);
+                    }
+                }
     }
-    __syncthreads();
-    if (wave != 0) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) sum[i] += __shfl_xor(sum[i], d);
+        if (lane == 0 && e0 + i * STEP < P.experts) logits[e0 + i * STEP] = sum[i] + bias[i];
+    }
+}
+// A wavefront's choice for a token: lane j gets choice j and its gate.
+__device__ __forceinline__ void choose_experts(const Moe& P, const float* logits, int& expert, float& gate) {
     constexpr int N = kMoeMaxExperts / 64;
+    const int lane = threadIdx.x & 63;
     float top = -INFINITY, sum = 0.f;
     uint32_t key[N];
 #pragma unroll
@@ -193,8 +207,9 @@ __global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
-    float mine = 0.f, chosen = 0.f;                  // lane j keeps choice j
-    int expert = -1;
+    float chosen = 0.f;
+    expert = -1;
+    gate = 0.f;
     for (int j = 0; j < P.top_k; ++j) {
         unsigned long long best = 0;
 #pragma unroll
@@ -214,11 +229,26 @@ __global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
             if (i * 64 + lane == e) key[i] = 0;
         const float g = expf(logits[e] - top) / sum;
         chosen += g;
-        if (lane == j) { mine = g; expert = e; }
+        if (lane == j) { gate = g; expert = e; }
     }
+    if (expert >= 0 && P.renormalize) gate /= chosen;
+}
+
+// A workgroup takes a token: its wavefronts deal the experts among themselves, the first one chooses.
+constexpr int kRouterWaves = 16;
+template <typename T>
+__global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
+    __shared__ float logits[kMoeMaxExperts];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, token = blockIdx.x;
+    for (int e = wave; e < P.experts; e += kRouterWaves) router_logits<T, 1, 1>(P, token, e, logits);
+    __syncthreads();
+    if (wave != 0) return;
+    int expert;
+    float gate;
+    choose_experts(P, logits, expert, gate);
     if (lane < P.top_k) {
         P.choice[(size_t)token * P.top_k + lane] = expert;
-        P.gate[(size_t)token * P.top_k + lane] = expert >= 0 && P.renormalize ? mine / chosen : mine;
+        P.gate[(size_t)token * P.top_k + lane] = gate;
     }
 }
 
@@ -248,14 +278,38 @@ __device__ __forceinline__ void count_experts(const Moe& P, Chosen& C, int t0, i
     }
     __syncthreads();
 }
+// The same with the choice made here, by every workgroup for itself (one to four tokens, a wavefront each); the first workgroup
+// leaves it in memory.
+template <typename T>
+__device__ __forceinline__ void choose_and_count(const Moe& P, Chosen& C, float (*logits)[kMoeMaxExperts], bool leave) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int i = threadIdx.x; i < kMoeMaxExperts; i += kMoeWaves * 64) C.count[i] = 0;
+    for (int t = 0; t < P.n_tokens; ++t)
+        for (int e = wave; e < P.experts; e += 2 * kMoeWaves) router_logits<T, 2, kMoeWaves>(P, t, e, logits[t]);
+    __syncthreads();
+    if (wave < P.n_tokens) {
+        int expert;
+        float gate;
+        choose_experts(P, logits[wave], expert, gate);
+        if (lane < P.top_k) {
+            C.choice[wave * P.top_k + lane] = expert;
+            if (expert >= 0) atomicAdd(&C.count[expert], 1);
+            if (leave) {
+                P.choice[wave * P.top_k + lane] = expert;
+                P.gate[wave * P.top_k + lane] = gate;
+            }
+        }
+    }
+    __syncthreads();
+}
 // The a-th part: its expert (-1: there are fewer), its place among the expert's parts, the expert's slots and first block.  Every
 // wavefront for itself: a lane per expert, sums over the lanes before.
-struct Part { int e, place, n, block; };
+struct Part { int e, place, n, block, all; };      // all: how many parts there are
 __device__ __forceinline__ Part find_part(const Moe& P, const Chosen& C, int a) {
     const int lane = threadIdx.x & 63;
-    Part part{-1, 0, 0, 0};
+    Part part{-1, 0, 0, 0, 0};
     int parts = 0, blocks = 0;                 // of the experts before
-    for (int i = 0; i * 64 < P.experts && part.e < 0; ++i) {
+    for (int i = 0; i * 64 < P.experts; ++i) {
         const int n = C.count[i * 64 + lane], own = (n + kMoePart - 1) / kMoePart << 16 | (n + 15) / 16;
         int sum = own;
 #pragma unroll
@@ -276,6 +330,7 @@ __device__ __forceinline__ Part find_part(const Moe& P, const Chosen& C, int a) 
         parts += all >> 16;
         blocks += all & 0xffff;
     }
+    part.all = parts;
     return part;
 }
 // Slots of the part in order, by the first wavefront, a lane per token.
@@ -290,6 +345,61 @@ __device__ __forceinline__ void list_slots(const Moe& P, Chosen& C, const Part& 
         if (at >= 0 && i >= 0 && i < kMoePart) C.slot[i] = at;
     }
     __syncthreads();
+}
+
+// Outputs of a slot.  SHARED: workgroups of the same launch, on whichever XCD, write and read them: then by atomic operations of the
+// GPU's scope, which go past the XCDs' own caches (a fence would write those back and drop what they hold: with one a
+// workgroup the second layers of 32 experts took 194 us instead of 33).
+template <bool SHARED>
+__device__ __forceinline__ void put_slot(float* p, const floatx4& v) {
+    if constexpr (SHARED) {
+        unsigned long long u[2];
+        __builtin_memcpy(u, &v, 16);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) __hip_atomic_store(reinterpret_cast<unsigned long long*>(p) + i, u[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    } else {
+        *reinterpret_cast<floatx4*>(p) = v;
+    }
+}
+template <bool SHARED>
+__device__ __forceinline__ floatx4 get_slot(const float* p) {
+    if constexpr (!SHARED) return *reinterpret_cast<const floatx4*>(p);
+    unsigned long long u[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) u[i] = __hip_atomic_load(reinterpret_cast<const unsigned long long*>(p) + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    floatx4 v;
+    __builtin_memcpy(&v, u, 16);
+    return v;
+}
+// out[token] = sum over its choices, in their order, of gate * the slot's output; four channels.  `choice`: the token's.
+template <typename T, bool SHARED>
+__device__ __forceinline__ void combine(const Moe& P, const int* choice, int token, int c) {
+    floatx4 sum{0.f, 0.f, 0.f, 0.f};
+    const size_t slot0 = (size_t)token * P.top_k;
+    for (int j0 = 0; j0 < P.top_k; j0 += 4) {          // four outputs on their way together
+        floatx4 y[4];
+        float gate[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int at = min(j0 + j, P.top_k - 1);
+            y[j] = get_slot<SHARED>(P.slot_out + (slot0 + at) * P.cout_pad + c);
+            gate[j] = P.gate[slot0 + at];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j0 + j < P.top_k && choice[j0 + j] >= 0)           // (an empty place has no output)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) sum[q] = fmaf(gate[j], y[j][q], sum[q]);
+    }
+    T* const out = static_cast<T*>(P.out) + (size_t)token * P.cout + c;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (c + q < P.cout) store(out + q, sum[q]);
+}
+template <typename T>
+__global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 4, token = blockIdx.y;
+    if (c < P.cout) combine<T, false>(P, P.choice + (size_t)token * P.top_k, token, c);
 }
 
 // The product of R tiles of 16 channels of an expert (gated: R / 2 in either half) with a part of its slots: relu or gate of
@@ -309,7 +419,7 @@ template <typename T, typename W, int KIND, int R, int MOST>
 __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     typedef Operand<T, W> Op;
     constexpr int PE = Op::PE, V = Op::V, HALVES = KIND == kUpGated ? 2 : 1, CT = R / HALVES, PLANES = sizeof(T) == 2 ? 2 : 1;
-    constexpr bool DOWN = KIND == kDown, TWO = DOWN && PLANES == 2;
+    constexpr bool DOWN = KIND == kDown, TWO = DOWN && PLANES == 2, ADDS = DOWN && MOST == 1;      // ADDS: the slots' outputs up, too
     __shared__ Chosen C;
     __shared__ floatx4 red[kMoeWaves][R][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -317,9 +427,27 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     const int channels = DOWN ? P.cout : P.hidden, K = DOWN ? P.hidden : P.cin;
     const int o0 = blockIdx.x * (CT * 16), t0 = blockIdx.z * kMoeTokens, n_tok = min(kMoeTokens, P.n_tokens - t0);
     const int pieces = (K + 4 * PE - 1) / (4 * PE), whole = K / (4 * PE), hidden_pieces = (P.hidden + 4 * PE - 1) / (4 * PE);
-    count_experts(P, C, t0, n_tok);
+    if constexpr (DOWN || MOST > 1) {
+        count_experts(P, C, t0, n_tok);
+    } else {
+        if (P.route) choose_and_count<T>(P, C, reinterpret_cast<float(*)[kMoeMaxExperts]>(&red[0][0][0]), blockIdx.x == 0 && blockIdx.y == 0);
+        else count_experts(P, C, t0, n_tok);
+    }
     const Part part = find_part(P, C, blockIdx.y);
     const int e = part.e;
+    auto add_up = [&]() {
+        for (int i = tid; i < n_tok * (CT * 4); i += kMoeWaves * 64) {
+            const int t = i / (CT * 4), c = o0 + i % (CT * 4) * 4;
+            if (c < P.cout) combine<T, true>(P, C.choice + t * P.top_k, t0 + t, c);
+        }
+    };
+    if constexpr (ADDS) {
+        if (part.all == 0 && blockIdx.y == 0) add_up();    // no token has an expert
+    }
+    if constexpr (!DOWN && MOST == 1) {
+        if (blockIdx.x == 0 && blockIdx.y == 0)
+            for (int i = tid; i < P.down_tiles; i += kMoeWaves * 64) P.done[i] = 0;
+    }
     if (e < 0) return;
     // Addresses are a uniform base and 32 bits a lane, so that what is ahead costs no registers but its own.  Tile r: half r / CT,
     // channels 16 (r % CT) on; past the end the last channel again.
@@ -433,7 +561,7 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                 }
             }
             if constexpr (DOWN) {
-                if (c0 < P.cout_pad) *reinterpret_cast<floatx4*>(P.slot_out + (size_t)slot * P.cout_pad + c0) = sum[0];
+                if (c0 < P.cout_pad) put_slot<ADDS>(P.slot_out + (size_t)slot * P.cout_pad + c0, sum[0]);
             } else {
                 if (c0 >= hidden_pieces * 4 * PE) continue;
                 T high[4], rest[4];
@@ -459,56 +587,61 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     };
     if (MOST == 1 || n <= 16) product(std::integral_constant<int, 1>());
     else product(std::integral_constant<int, 2>());
-}
-
-// out[token] = sum over its choices of gate * the slot's output
-template <typename T>
-__global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 4, token = blockIdx.y;
-    if (c >= P.cout) return;
-    floatx4 sum{0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < P.top_k; ++j) {
-        const size_t slot = (size_t)token * P.top_k + j;
-        if (P.choice[slot] < 0) break;                         // (the places behind it are empty too)
-        const floatx4 y = *reinterpret_cast<const floatx4*>(P.slot_out + slot * P.cout_pad + c);
-        const float gate = P.gate[slot];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] = fmaf(gate, y[i], sum[i]);
+    if constexpr (ADDS) {
+        // The workgroup that comes last for these channels adds up; nothing waits for another.
+        __shared__ int last;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");      // this wavefront's outputs have arrived
+        __syncthreads();
+        if (tid == 0) last = __hip_atomic_fetch_add(P.done + blockIdx.x, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == part.all - 1;
+        __syncthreads();
+        if (last) add_up();
     }
-    T* const out = static_cast<T*>(P.out) + (size_t)token * P.cout + c;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (c + i < P.cout) store(out + i, sum[i]);
 }
 
 template <typename T, typename W, int KIND, int R>
-hipError_t expert_launch_as(const Moe& P, unsigned tiles, unsigned active, hipStream_t st) {
-    const dim3 grid(tiles, active, (unsigned)((P.n_tokens + kMoeTokens - 1) / kMoeTokens)), block(kMoeWaves * 64);
+hipError_t expert_launch_as(const Moe& P, unsigned tiles, unsigned parts, hipStream_t st) {
+    const dim3 grid(tiles, parts, (unsigned)((P.n_tokens + kMoeTokens - 1) / kMoeTokens)), block(kMoeWaves * 64);
     if (P.n_tokens <= 16) hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 1>), grid, block, 0, st, P);
     else hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 2>), grid, block, 0, st, P);
     return hipGetLastError();
 }
-// As many tiles of channels a workgroup as leave a workgroup for every CU.
+// Tiles of channels a workgroup: more of them share a fragment of the rows, fewer give more workgroups.  Few tokens have one fragment
+// and want four workgroups a CU (us, four tiles -> fewer: 1024 -> 2048 -> 1024 fp32 16 rows 22.7 + 25.8 -> 20.7 + 22.8), more want the sharing
+// as long as there is one for every CU (8192 -> 4096 in 8 bits 64 rows 80 -> 95).
+struct Shape { int tiles; unsigned wgs; };
+Shape shape_of(const Moe& P, int channels, int halves, unsigned parts) {
+    const unsigned want = P.n_tokens <= 16 ? 1024 : 256;
+    for (int r = 4; r >= halves; r >>= 1) {
+        const unsigned wgs = (unsigned)(channels + 16 * r / halves - 1) / (16 * r / halves);
+        if (wgs * parts >= want || r == halves) return Shape{r, wgs};
+    }
+    return Shape{halves, 0};       // (not reached)
+}
 template <typename T, typename W, int KIND>
-hipError_t expert_launch(const Moe& P, hipStream_t st) {
-    const int slots = std::min(P.n_tokens, kMoeTokens) * P.top_k;
-    const unsigned active = (unsigned)(std::min(P.experts, slots) + (P.n_tokens > kMoePart ? slots / (kMoePart + 1) : 0));      // parts, at most
-    constexpr unsigned kHalves = KIND == kUpGated ? 2 : 1, kPiece = 64 / sizeof(W);
-    const unsigned channels = KIND == kDown ? (unsigned)P.cout : ((unsigned)P.hidden + kPiece - 1) / kPiece * kPiece;      // (whole pieces of hidden values)
-    auto tiles = [&](unsigned r) { return (channels + 16 * r / kHalves - 1) / (16 * r / kHalves); };
-    if (tiles(4) * active >= 256) return expert_launch_as<T, W, KIND, 4>(P, tiles(4), active, st);
-    if constexpr (kHalves == 1)
-        if (tiles(2) * active < 256) return expert_launch_as<T, W, KIND, 1>(P, tiles(1), active, st);
-    return expert_launch_as<T, W, KIND, 2>(P, tiles(2), active, st);
+hipError_t expert_launch(const Moe& P, const Shape& s, unsigned parts, hipStream_t st) {
+    if (s.tiles == 4) return expert_launch_as<T, W, KIND, 4>(P, s.wgs, parts, st);
+    if constexpr (KIND != kUpGated)
+        if (s.tiles == 1) return expert_launch_as<T, W, KIND, 1>(P, s.wgs, parts, st);
+    return expert_launch_as<T, W, KIND, 2>(P, s.wgs, parts, st);
 }
 
 template <typename T, typename W>
-hipError_t moe_run(const Moe& P, bool gated, hipStream_t st) {
-    hipLaunchKernelGGL((moe_choose_kernel<T>), dim3((unsigned)P.n_tokens), dim3(kRouterWaves * 64), 0, st, P);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess) e = gated ? expert_launch<T, W, kUpGated>(P, st) : expert_launch<T, W, kUpRelu>(P, st);
-    if (e == hipSuccess) e = expert_launch<T, W, kDown>(P, st);
-    if (e != hipSuccess) return e;
+hipError_t moe_run(Moe& P, bool gated, hipStream_t st) {
+    const int slots = std::min(P.n_tokens, kMoeTokens) * P.top_k;
+    const unsigned parts = (unsigned)(std::min(P.experts, slots) + (P.n_tokens > kMoePart ? slots / (kMoePart + 1) : 0));      // at most
+    constexpr int kPiece = 64 / sizeof(W);
+    const Shape up = shape_of(P, (P.hidden + kPiece - 1) / kPiece * kPiece, gated ? 2 : 1, parts);       // (whole pieces of hidden values)
+    const Shape down = shape_of(P, P.cout, 1, parts);
+    P.down_tiles = (int)down.wgs;
+    P.route = P.n_tokens <= kMoeWaves && P.experts <= 16 && P.cin * (int)sizeof(T) <= 16384;
+    hipError_t e = hipSuccess;
+    if (!P.route) {
+        hipLaunchKernelGGL((moe_choose_kernel<T>), dim3((unsigned)P.n_tokens), dim3(kRouterWaves * 64), 0, st, P);
+        e = hipGetLastError();
+    }
+    if (e == hipSuccess) e = gated ? expert_launch<T, W, kUpGated>(P, up, parts, st) : expert_launch<T, W, kUpRelu>(P, up, parts, st);
+    if (e == hipSuccess) e = expert_launch<T, W, kDown>(P, down, parts, st);
+    if (e != hipSuccess || P.n_tokens <= 16) return e;
     hipLaunchKernelGGL((moe_combine_kernel<T>), dim3((unsigned)((P.cout + 1023) / 1024), (unsigned)P.n_tokens), dim3(256), 0, st, P);
     return hipGetLastError();
 }
@@ -516,7 +649,7 @@ hipError_t moe_run(const Moe& P, bool gated, hipStream_t st) {
 }  // namespace
 
 // The workspace: the choice (where the caller does not take it), the hidden values and the outputs of every slot.
-struct MoeSpace { size_t gate, hidden, slots, end; };
+struct MoeSpace { size_t gate, hidden, slots, done, end; };
 static size_t group_blocks(const dc_moe& m, int n_tokens) {
     const int tokens = std::min(n_tokens, kMoeTokens);
     return ((size_t)tokens * m.top_k + 15 * (size_t)std::min(m.experts, tokens * m.top_k)) / 16;
@@ -528,7 +661,8 @@ static MoeSpace moe_space(const dc_moe& m, int n_tokens) {
     s.hidden = 2 * s.gate;
     // (rows of the type's own size or two of half of it; an expert's last block is not full)
     s.slots = s.hidden + ((size_t)n_tokens + kMoeTokens - 1) / kMoeTokens * group_blocks(m, n_tokens) * 16 * align_up(m.hidden, 64) * 4;
-    s.end = s.slots + align_up(slots * align_up(m.cout, 4) * 4, 256);
+    s.done = s.slots + align_up(slots * align_up(m.cout, 4) * 4, 256);
+    s.end = s.done + align_up((size_t)((m.cout + 15) / 16) * 4, 256);
     return s;
 }
 size_t moe_workspace(const dc_moe& m, int n_tokens) { return moe_space(m, n_tokens).end; }
@@ -546,6 +680,7 @@ hipError_t launch_moe(const dc_moe& m, const dc_moe_weights& w, const void* in, 
     P.gate = gates ? gates : reinterpret_cast<float*>(base + space.gate);
     P.hidden_out = base + space.hidden;
     P.slot_out = reinterpret_cast<float*>(base + space.slots);
+    P.done = reinterpret_cast<int32_t*>(base + space.done);
     P.n_tokens = n_tokens; P.experts = m.experts; P.top_k = m.top_k; P.cin = m.cin; P.hidden = m.hidden; P.cout = m.cout;
     P.renormalize = m.renormalize; P.group_blocks = (int)group_blocks(m, n_tokens); P.cout_pad = (int)align_up(m.cout, 4);
     const bool gated = m.act == DC_MOE_GATED;
