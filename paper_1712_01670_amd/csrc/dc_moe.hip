@@ -30,6 +30,7 @@ struct Moe {
     unsigned char* hidden_out;         // the experts' hidden values, in blocks of 16 slots (Chosen)
     int n_tokens, experts, top_k, cin, hidden, cout, renormalize;
     int group_blocks, cout_pad;        // blocks of a group of tokens; cout rounded up to 4
+    int block_rows;                    // rows of a block of hidden values: 16, or 4 / 8 if there are no more tokens
     float* slot_out;                   // [n_tokens * top_k][cout_pad]: the experts' outputs
     int32_t* done;                     // [down_tiles], up to 16 tokens: workgroups of the second layers that have written theirs
     int down_tiles, route;             // route: the first layers' kernel makes the choice itself
@@ -255,7 +256,8 @@ __global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
 // ---- the experts ----------------------------------------------------------------------------------------------------------
 // The slots (token * top_k + choice) of a group of kMoeTokens tokens, by expert.  Every workgroup finds its own: the choices are a few
 // hundred numbers.  An expert's slots are dealt in parts of 32, a workgroup each; the hidden values of its i-th slot stand in
-// row i % 16 of block base + i / 16, base being the blocks of the experts before.
+// row i % 16 of block base + i / 16, base being the blocks of the experts before (a block has fewer rows if there are no more
+// tokens: what a wavefront fetches of it is whole).
 constexpr int kMoePart = 32;
 struct Chosen {
     int count[kMoeMaxExperts];             // slots of an expert
@@ -405,7 +407,7 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
 // The product of R tiles of 16 channels of an expert (gated: R / 2 in either half) with a part of its slots: relu or gate of
 // the first layer into the hidden values, or the second layer into the slots' outputs.  The weights are what has to come from
 // memory, once: they go straight into operands (16 rows of 64 bytes an instruction), three pieces of a wavefront
-// ahead, and K is dealt among the wavefronts by pairs of pieces, whole cache lines; their sums are added through LDS in a fixed
+// ahead, and every wavefront takes a run of K, of whole cache lines; their sums are added through LDS in a fixed
 // order.  The tokens' rows come from L2, a piece ahead, once for R tiles of weights: a row of a fragment costs the CU a look-up for
 // every 16 bytes, as a row of weights does, so R is large where there are workgroups enough.  The hidden values lie in the order
 // of the second layer's fragments, 1 KiB a look-up of 16, fp32 or as two bf16 numbers each (the value's rounding and what
@@ -427,6 +429,7 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     const int channels = DOWN ? P.cout : P.hidden, K = DOWN ? P.hidden : P.cin;
     const int o0 = blockIdx.x * (CT * 16), t0 = blockIdx.z * kMoeTokens, n_tok = min(kMoeTokens, P.n_tokens - t0);
     const int pieces = (K + 4 * PE - 1) / (4 * PE), whole = K / (4 * PE), hidden_pieces = (P.hidden + 4 * PE - 1) / (4 * PE);
+    const int piece_bytes = P.block_rows * (V * 64);       // of a block of hidden values
     if constexpr (DOWN || MOST > 1) {
         count_experts(P, C, t0, n_tok);
     } else {
@@ -458,41 +461,56 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
         wbase[h] = reinterpret_cast<const unsigned char*>(static_cast<const W*>(DOWN ? P.down : P.up) + (((size_t)e * HALVES + h) * channels + o0) * K);
 #pragma unroll
     for (int c = 0; c < CT; ++c) wat[c] = (uint32_t)max(0, min(c * 16 + l16, channels - 1 - o0)) * (uint32_t)(K * sizeof(W)) + g * 16;
-    auto at = [&](int i) { return (wave + i / 2 * kMoeWaves) * 2 + i % 2; };       // piece i of this wavefront
+    const int share = ((whole + 1) / 2 + kMoeWaves - 1) / kMoeWaves * 2, first = wave * share, end = min(whole, first + share);      // this wavefront's pieces
     uintx4 w[4][R];
     auto fetch_w = [&](uintx4 (&to)[R], int p) {
-        if (p < whole)
+        if (p < end)
 #pragma unroll
             for (int r = 0; r < R; ++r) to[r] = load16(wbase[r / CT] + (uint32_t)(p * 64) + wat[r % CT]);
     };
 #pragma unroll
-    for (int d = 0; d < 3; ++d) fetch_w(w[d], at(d));
+    for (int d = 0; d < 3; ++d) fetch_w(w[d], first + d);
+    floatx4 scale[HALVES], bias[HALVES];                   // of the channels that this wavefront finishes
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            scale[h][q] = 1.f;
+            bias[h][q] = 0.f;
+            if (wave < CT) {
+                const size_t c = ((size_t)e * HALVES + h) * channels + min(o0 + wave * 16 + g * 4 + q, channels - 1);
+                if constexpr (sizeof(W) == 1) scale[h][q] = (DOWN ? P.down_scale : P.up_scale)[c];
+                const float* const b = DOWN ? P.down_bias : P.up_bias;
+                if (b) bias[h][q] = b[c];
+            }
+        }
     list_slots(P, C, part, t0, n_tok);                     // (while the first weights travel)
     const int n = min(kMoePart, part.n - part.place * kMoePart);
-    unsigned char* const tiles = P.hidden_out + ((size_t)blockIdx.z * P.group_blocks + part.block + part.place * (kMoePart / 16)) * PLANES * hidden_pieces * (V * 1024);
+    unsigned char* const tiles = P.hidden_out + ((size_t)blockIdx.z * P.group_blocks + part.block + part.place * (kMoePart / 16)) * PLANES * hidden_pieces * piece_bytes;
     auto product = [&](auto blocks) {                      // of 16 slots
         constexpr int NB = decltype(blocks)::value;
         const unsigned char* xbase[DOWN ? NB : 1];
         uint32_t xat[DOWN ? 1 : NB];
         if constexpr (DOWN) {
-            xat[0] = lane * 16;
+            xat[0] = (g * P.block_rows + (NB == 1 ? min(l16, n - 1) : l16)) * 16;      // (rows that are not there repeat the last one)
 #pragma unroll
-            for (int j = 0; j < NB; ++j) xbase[j] = tiles + (size_t)j * PLANES * hidden_pieces * (V * 1024);
+            for (int j = 0; j < NB; ++j) xbase[j] = tiles + (size_t)j * PLANES * hidden_pieces * piece_bytes;
         } else {
             xbase[0] = static_cast<const unsigned char*>(P.x);
 #pragma unroll
             for (int j = 0; j < NB; ++j) xat[j] = (uint32_t)(C.slot[min(j * 16 + l16, n - 1)] / P.top_k) * (uint32_t)(P.cin * sizeof(T));
         }
-        Op x[2][NB], low[2][TWO ? NB : 1];
+        constexpr int XRING = MOST == 1 ? 4 : 2, XAHEAD = XRING / 2;       // rows of few tokens are small enough for two pieces ahead
+        Op x[XRING][NB], low[XRING][TWO ? NB : 1];
         auto fetch_x = [&](int b, int p, bool end = false, int k0 = 0) {
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 if constexpr (DOWN) {
 #pragma unroll
                     for (int v = 0; v < V; ++v) {
-                        const unsigned char* const from = xbase[j] + (uint32_t)((p * V + v) * 1024);
+                        const unsigned char* const from = xbase[j] + (uint32_t)(p * piece_bytes + v * (piece_bytes / V));
                         x[b][j].v[v] = load16(from + xat[0]);
-                        if constexpr (TWO) low[b][j].v[v] = load16(from + (uint32_t)(hidden_pieces * (V * 1024)) + xat[0]);
+                        if constexpr (TWO) low[b][j].v[v] = load16(from + (uint32_t)(hidden_pieces * piece_bytes) + xat[0]);
                     }
                 } else if (end) {
                     x[b][j].load_end(reinterpret_cast<const T*>(xbase[0] + xat[j]), k0, K);
@@ -520,18 +538,20 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                 }
             }
         };
-        if (at(0) < whole) fetch_x(0, at(0));
-        for (int i = 0; at(i) < whole; i += 4) {
+#pragma unroll
+        for (int d = 0; d < XAHEAD; ++d)
+            if (first + d < end) fetch_x(d, first + d);
+        for (int p = first; p < end; p += 4) {
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                if (at(i + d + 1) < whole) fetch_x((d + 1) & 1, at(i + d + 1));      // (loads come back in order: the rows before the
-                fetch_w(w[(d + 3) & 3], at(i + d + 3));                                     // weights further ahead)
+                if (p + d + XAHEAD < end) fetch_x((d + XAHEAD) % XRING, p + d + XAHEAD);       // (loads come back in order: the rows
+                fetch_w(w[(d + 3) & 3], p + d + 3);                                            // before the weights further ahead)
                 __builtin_amdgcn_sched_barrier(0);
-                if (at(i + d) < whole) multiply(w[d], d & 1);
+                if (p + d < end) multiply(w[d], d % XRING);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
-        if (pieces > whole && wave == whole / 2 % kMoeWaves) {         // the piece that K ends in
+        if (pieces > whole && wave == kMoeWaves - 1) {         // the piece that K ends in
             const int k0 = opaque(whole * (4 * PE) + g * PE);
 #pragma unroll
             for (int r = 0; r < R; ++r) w[0][r] = load16_end(reinterpret_cast<const W*>(wbase[r / CT] + (wat[r % CT] - g * 16)), k0, K);
@@ -554,11 +574,7 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
 #pragma unroll
                 for (int v = 1; v < kMoeWaves; ++v) sum[h] += red[v][h * CT + ct][lane];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const size_t c = ((size_t)e * HALVES + h) * channels + min(c0 + q, channels - 1);
-                    const float* const bias = DOWN ? P.down_bias : P.up_bias;
-                    sum[h][q] = sum[h][q] * (sizeof(W) == 1 ? (DOWN ? P.down_scale : P.up_scale)[c] : 1.f) + (bias ? bias[c] : 0.f);
-                }
+                for (int q = 0; q < 4; ++q) sum[h][q] = fmaf(sum[h][q], scale[h][q], bias[h][q]);
             }
             if constexpr (DOWN) {
                 if (c0 < P.cout_pad) put_slot<ADDS>(P.slot_out + (size_t)slot * P.cout_pad + c0, sum[0]);
@@ -578,10 +594,10 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                 }
                 // channel c0 is element c0 % PE of lane group c0 / PE % 4 of piece c0 / (4 PE)
                 constexpr int VE = 16 / sizeof(T);
-                unsigned char* const to = tiles + (size_t)j * PLANES * hidden_pieces * (V * 1024) +
-                                          ((size_t)(c0 / (4 * PE)) * V + c0 % PE / VE) * 1024 + (c0 / PE % 4 * 16 + l16) * 16 + c0 % VE * sizeof(T);
+                unsigned char* const to = tiles + (size_t)j * PLANES * hidden_pieces * piece_bytes + (size_t)(c0 / (4 * PE)) * piece_bytes +
+                                          c0 % PE / VE * (piece_bytes / V) + (c0 / PE % 4 * P.block_rows + l16) * 16 + c0 % VE * sizeof(T);
                 __builtin_memcpy(__builtin_assume_aligned(to, 4 * sizeof(T)), high, sizeof high);
-                if constexpr (PLANES == 2) __builtin_memcpy(__builtin_assume_aligned(to + (size_t)hidden_pieces * (V * 1024), 4 * sizeof(T)), rest, sizeof rest);
+                if constexpr (PLANES == 2) __builtin_memcpy(__builtin_assume_aligned(to + (size_t)hidden_pieces * piece_bytes, 4 * sizeof(T)), rest, sizeof rest);
             }
         }
     };
@@ -650,6 +666,7 @@ hipError_t moe_run(Moe& P, bool gated, hipStream_t st) {
 
 // The workspace: the choice (where the caller does not take it), the hidden values and the outputs of every slot.
 struct MoeSpace { size_t gate, hidden, slots, done, end; };
+static int block_rows(int n_tokens) { return n_tokens <= 4 ? 4 : n_tokens <= 8 ? 8 : 16; }
 static size_t group_blocks(const dc_moe& m, int n_tokens) {
     const int tokens = std::min(n_tokens, kMoeTokens);
     return ((size_t)tokens * m.top_k + 15 * (size_t)std::min(m.experts, tokens * m.top_k)) / 16;
@@ -660,7 +677,7 @@ static MoeSpace moe_space(const dc_moe& m, int n_tokens) {
     s.gate = align_up(slots * 4, 256);
     s.hidden = 2 * s.gate;
     // (rows of the type's own size or two of half of it; an expert's last block is not full)
-    s.slots = s.hidden + ((size_t)n_tokens + kMoeTokens - 1) / kMoeTokens * group_blocks(m, n_tokens) * 16 * align_up(m.hidden, 64) * 4;
+    s.slots = s.hidden + ((size_t)n_tokens + kMoeTokens - 1) / kMoeTokens * group_blocks(m, n_tokens) * block_rows(n_tokens) * align_up(m.hidden, 64) * 4;
     s.done = s.slots + align_up(slots * align_up(m.cout, 4) * 4, 256);
     s.end = s.done + align_up((size_t)((m.cout + 15) / 16) * 4, 256);
     return s;
@@ -682,7 +699,7 @@ hipError_t launch_moe(const dc_moe& m, const dc_moe_weights& w, const void* in, 
     P.slot_out = reinterpret_cast<float*>(base + space.slots);
     P.done = reinterpret_cast<int32_t*>(base + space.done);
     P.n_tokens = n_tokens; P.experts = m.experts; P.top_k = m.top_k; P.cin = m.cin; P.hidden = m.hidden; P.cout = m.cout;
-    P.renormalize = m.renormalize; P.group_blocks = (int)group_blocks(m, n_tokens); P.cout_pad = (int)align_up(m.cout, 4);
+    P.renormalize = m.renormalize; P.group_blocks = (int)group_blocks(m, n_tokens); P.block_rows = block_rows(n_tokens); P.cout_pad = (int)align_up(m.cout, 4);
     const bool gated = m.act == DC_MOE_GATED;
     if (dtype == DC_BF16) return m.wtype == DC_I8 ? moe_run<uint16_t, int8_t>(P, gated, st) : moe_run<uint16_t, uint16_t>(P, gated, st);
     return m.wtype == DC_I8 ? moe_run<float, int8_t>(P, gated, st) : moe_run<float, float>(P, gated, st);
