@@ -217,10 +217,12 @@ def _fc_quant_bytes(n, K, cout):
 
 
 @functools.lru_cache(maxsize=256)
-def _moe_bytes(*fields):
-    need = C.c_size_t()
-    _check("dc_moe_workspace_bytes", lib().dc_moe_workspace_bytes(C.byref(Moe(*fields[:-1])), fields[-1], C.byref(need)))
-    return need.value
+def _moe_of(n, experts, top_k, cin, hidden, cout, act, renormalize, wtype):
+    """(dc_moe, workspace bytes, shapes of the tensors) of a call on n tokens."""
+    m, need = Moe(experts, top_k, cin, hidden, cout, act, int(renormalize), wtype), C.c_size_t()
+    _check("dc_moe_workspace_bytes", lib().dc_moe_workspace_bytes(C.byref(m), n, C.byref(need)))
+    rows = hidden * (2 if act == DC_MOE_GATED else 1)
+    return m, need.value, ((n, cin), (experts, cin), (experts, rows, cin), (experts, cout, hidden), (n, top_k), (experts,))
 
 
 def _scratch(n_bytes, device):
@@ -600,27 +602,29 @@ def dc_moe_layer(moe, x, router, up, down, router_bias=None, up_bias=None, down_
     (dc_quantize_rows); biases fp32 or None.  Returns (out [n][cout], experts int32 [n][top_k], gates fp32 [n][top_k])."""
     fn = "dc_moe_layer"
     dtype = _rows_dtype(fn, x)
-    E, k, cin, hidden, cout = (int(moe[f]) for f in ("experts", "top_k", "cin", "hidden", "cout"))
-    act = int(moe["act"])
-    rows = hidden * (2 if act == DC_MOE_GATED else 1)
-    int8 = up.dtype == torch.int8
     dev, n = x.device, x.shape[0]
-    _want(fn, x, x.dtype, (n, cin), dev)
-    _want(fn, router, x.dtype, (E, cin), dev)
-    _want(fn, up, torch.int8 if int8 else x.dtype, (E, rows, cin), dev)
-    _want(fn, down, up.dtype, (E, cout, hidden), dev)
-    for t, shape in ((router_bias, (E,)), (up_bias, (E, rows)), (down_bias, (E, cout)), (up_scale, (E, rows)), (down_scale, (E, cout))):
+    weights_type = up.dtype
+    m, need, shapes = _moe_of(n, moe["experts"], moe["top_k"], moe["cin"], moe["hidden"], moe["cout"], moe["act"], moe["renormalize"],
+                              DC_I8 if weights_type == torch.int8 else dtype)
+    if weights_type != torch.int8:
+        weights_type = x.dtype
+    x_shape, router_shape, up_shape, down_shape, gates_shape, bias_shape = shapes
+    _want(fn, x, x.dtype, x_shape, dev)
+    _want(fn, router, x.dtype, router_shape, dev)
+    _want(fn, up, weights_type, up_shape, dev)
+    _want(fn, down, weights_type, down_shape, dev)
+    for t, shape in ((router_bias, bias_shape), (up_bias, up_shape[:2]), (down_bias, down_shape[:2]), (up_scale, up_shape[:2]), (down_scale, down_shape[:2])):
         if t is not None:
             _want(fn, t, torch.float32, shape, dev)
-    m = Moe(E, k, cin, hidden, cout, act, int(moe["renormalize"]), DC_I8 if int8 else dtype)
-    need = _moe_bytes(E, k, cin, hidden, cout, act, m.renormalize, m.wtype, n)
-    p = [t.data_ptr() if t is not None else None for t in (router, router_bias, up, up_scale, up_bias, down, down_scale, down_bias)]
+    w = MoeWeights(router.data_ptr(), None if router_bias is None else router_bias.data_ptr(),
+                   up.data_ptr(), None if up_scale is None else up_scale.data_ptr(), None if up_bias is None else up_bias.data_ptr(),
+                   down.data_ptr(), None if down_scale is None else down_scale.data_ptr(), None if down_bias is None else down_bias.data_ptr())
     with _on(dev):
-        out = x.new_empty((n, cout))
-        experts = torch.empty((n, k), dtype=torch.int32, device=dev)
-        gates = torch.empty((n, k), dtype=torch.float32, device=dev)
+        out = x.new_empty((n, moe["cout"]))
+        experts = torch.empty(gates_shape, dtype=torch.int32, device=dev)
+        gates = torch.empty(gates_shape, dtype=torch.float32, device=dev)
         ws = _scratch(need, dev)
-        _check(fn, lib().dc_moe_layer(C.byref(m), C.byref(MoeWeights(*p)), x.data_ptr(), out.data_ptr(), experts.data_ptr(), gates.data_ptr(),
+        _check(fn, lib().dc_moe_layer(m, C.byref(w), x.data_ptr(), out.data_ptr(), experts.data_ptr(), gates.data_ptr(),
                                       n, dtype, ws.data_ptr(), need, _raw_stream(dev)))
     return out, experts, gates
 

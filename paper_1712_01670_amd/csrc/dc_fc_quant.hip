@@ -572,10 +572,16 @@ hipError_t product_few(const FcI8& P, hipStream_t st) {
     if (P.n_rows <= 48) return rows_launch<T, 3, 8, 2, false>(P, st);
     return rows_launch<T, 4, 8, 2, false>(P, st);
 }
+// us, 128 x 128 (two workgroups a CU) against 256 x 256: 4096 -> 4096 on 16384 rows (4096 or 1024 tiles) 277 against 265, 2048 -> 2048
+// on 8192 (1024 or 256) 45 against 52.  Three stages in flight are worth one workgroup a CU while there are no more tiles than CUs: 4096 ->
+// 4096 on 1024 rows 26.4 -> 22.2, but 2048 -> 2048 on 4096 (512 tiles) 24.1 -> 28.8.  Half as many tiles or fewer leave CUs idle:
+// 4096 -> 4096 on 256 rows 17.7 with 128 x 128, 10.4 with 64 x 64 (four stages; two 11.2).  Up to 64 channels: 256 -> 64 on 50176
+// rows 6.7 with 128 x 64, 8.4 with 128 x 128, 7.3 with 64 x 64.
 template <typename T>
 hipError_t product_many(const FcI8& P, hipStream_t st) {
-    const long tiles = ((long)P.n_rows + 127) / 128 * ((P.cout + 127) / 128);
+    const long tiles = ((long)P.n_rows + 127) / 128 * ((P.cout + 127) / 128), big = ((long)P.n_rows + 255) / 256 * ((P.cout + 255) / 256);
     if (P.cout <= 64 && tiles > 64) return gemm<T, 8, 4, 2, 4, 2>(P, st);
+    if (big >= 768) return gemm<T, 16, 16, 2, 4, 2>(P, st);
     if (tiles > 256) return gemm<T, 8, 8, 2, 4, 2>(P, st);
     if (tiles > 128) return gemm<T, 8, 8, 2, 4, 3>(P, st);
     return gemm<T, 4, 4, 2, 4, 4>(P, st);
