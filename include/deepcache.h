@@ -494,7 +494,7 @@ int32_t dc_softmax_layer(const void* in, void* out, size_t n_pixels, int32_t C, 
  * an infinity has the scale NaN and zeros, so that every product with it is NaN.  Scales among the subnormal
  * numbers (rows below 1e-36) are coarse; q then saturates at +-127.
  *   in      dev [n_rows][K] in `dtype`;  q  dev int8 [n_rows][K];  scales  dev fp32 [n_rows].  No alignment is asked for
- *           beyond the types' own.  1 <= K <= 131072.
+ *           beyond the types' own.  1 <= K <= 131072, n_rows < 2^31.  q must not overlap `in`.
  */
 int32_t dc_quantize_rows(const void* in, size_t n_rows, size_t K, int32_t dtype, int8_t* q, float* scales, void* stream);
 
@@ -508,12 +508,22 @@ int32_t dc_quantize_rows(const void* in, size_t n_rows, size_t K, int32_t dtype,
  *   weights   dev int8 [cout][K], weight_scales dev fp32 [cout], bias dev fp32 [cout] or NULL
  *   ws_dev    dev workspace of at least dc_fc_quant_workspace_bytes, 256-byte aligned; calls that may overlap in time need
  *             workspaces of their own
- * 1 <= K <= 131072 (the sum fits 32 bits).  relu: 0 or 1; a NaN stays one.  Rows with a NaN or an infinity give NaN rows.
+ * 1 <= K <= 131072 (the sum fits 32 bits); n_rows <= 2^24, cout <= 2^20, n_rows * cout <= 2^34.  relu: 0 or 1; a NaN stays one.
+ * Rows with a NaN or an infinity give NaN rows.
  */
 int32_t dc_fc_quant_workspace_bytes(int32_t n_rows, size_t K, int32_t cout, size_t* bytes);
 int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* weight_scales, const float* bias, void* out,
                        int32_t n_rows, size_t K, int32_t cout, int32_t relu, int32_t dtype,
                        void* ws_dev, size_t ws_dev_bytes, void* stream);
+
+/*
+ * The same weights in one block, for the fully-connected layers of a stack: int8 [cout][K] and, from the next multiple of 16
+ * bytes on, their fp32 scales [cout].  A block passed to dc_run_stack as the packed_weights entry of a DC_FC layer makes the
+ * layer run as dc_fc_quant_layer does, with the plain weights unused.
+ *   weights dev [cout][K] in `dtype`, packed dev, 16-byte aligned, dc_packed_fc_bytes long
+ */
+int32_t dc_packed_fc_bytes(size_t K, int32_t cout, size_t* bytes);
+int32_t dc_pack_fc_weights(const void* weights, size_t K, int32_t cout, int32_t dtype, void* packed, void* stream);
 
 /*
  * Mixture-of-experts layer for a few tokens (a row of features per stream): a router chooses top_k of `experts` pairs of
@@ -569,7 +579,9 @@ int32_t dc_stack_workspace_bytes(const dc_layer* layers, int32_t n_layers, int32
  * pooling / add / ReLU layers computed in full.
  *   weights, bias   host arrays [n_layers] of dev pointers (NULL for non-conv layers)
  *   packed_weights  optional (NULL) host array [n_layers] of dev pointers: packed copies of the
- *                   weights (NULL entries for layers without one)
+ *                   weights (NULL entries for layers without one); a DC_FC layer's entry is a block of
+ *                   dc_pack_fc_weights and makes it a layer in 8-bit integers (its rows of up to 131072
+ *                   values are rounded into the scratch areas of ws_dev: DC_ERR_WORKSPACE if they do not fit)
  *   frames_cur      dev u8 [n_streams][H][W][C]
  *   frames_prev     dev u8, previous frames (cache keys); ignored when force_full
  *   tensors_cur     host array [n_layers+1] of dev pointers, every tensor of this frame

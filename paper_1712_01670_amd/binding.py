@@ -32,7 +32,7 @@ EXPORTS = ["dc_status_string", "dc_profile_create", "dc_profile_destroy", "dc_pr
            "dc_stack_workspace_bytes", "dc_run_stack", "dc_stack_stats_fetch", "dc_cached_conv_layer_noalloc",
            "dc_propagate_masks_size", "dc_propagate_masks", "dc_probe_mfma_rate",
            "dc_quantize_rows", "dc_fc_quant_workspace_bytes", "dc_fc_quant_layer",
-           "dc_moe_workspace_bytes", "dc_moe_layer"]
+           "dc_packed_fc_bytes", "dc_pack_fc_weights", "dc_moe_workspace_bytes", "dc_moe_layer"]
 
 
 class DcError(RuntimeError):
@@ -134,6 +134,8 @@ def lib():
         L.dc_quantize_rows.argtypes = [vp, sz, sz, i32, vp, vp, vp]
         L.dc_fc_quant_workspace_bytes.argtypes = [i32, sz, i32, C.POINTER(sz)]
         L.dc_fc_quant_layer.argtypes = [vp, vp, vp, vp, vp, i32, sz, i32, i32, i32, vp, sz, vp]
+        L.dc_packed_fc_bytes.argtypes = [sz, i32, C.POINTER(sz)]
+        L.dc_pack_fc_weights.argtypes = [vp, sz, i32, i32, vp, vp]
         L.dc_moe_workspace_bytes.argtypes = [C.POINTER(Moe), i32, C.POINTER(sz)]
         L.dc_moe_layer.argtypes = [C.POINTER(Moe), C.POINTER(MoeWeights), vp, vp, vp, vp, i32, i32, vp, sz, vp]
         L.dc_stack_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32, i32, i32, C.POINTER(sz), C.POINTER(sz)]
@@ -567,12 +569,25 @@ def dc_quantize_rows(x):
     """8-bit form of the rows of x [..., K] (cuda, fp32 or bf16): (int8 tensor of x's shape, fp32 scales of its leading shape).
     A matrix of weights [cout][K] becomes the weights of dc_fc_quant_layer."""
     dtype = _rows_dtype("dc_quantize_rows", x)
-    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
-    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     with _on(x.device):
+        q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+        scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
         _check("dc_quantize_rows", lib().dc_quantize_rows(x.data_ptr(), scales.numel(), x.shape[-1], dtype, q.data_ptr(),
-                                                          scales.data_ptr(), _stream()))
+                                                          scales.data_ptr(), _raw_stream(x.device)))
     return q, scales
+
+
+def dc_pack_fc_weights(w):
+    """dc_quantize_rows of a fully-connected layer's weights [cout][...] (cuda, fp32 or bf16) in one block (uint8 tensor), as
+    dc_run_stack takes them."""
+    dtype = _rows_dtype("dc_pack_fc_weights", w)
+    cout = w.shape[0]
+    K, need = w.numel() // cout, C.c_size_t()
+    _check("dc_packed_fc_bytes", lib().dc_packed_fc_bytes(K, cout, C.byref(need)))
+    with _on(w.device):
+        packed = torch.empty(need.value, dtype=torch.uint8, device=w.device)
+        _check("dc_pack_fc_weights", lib().dc_pack_fc_weights(w.data_ptr(), K, cout, dtype, packed.data_ptr(), _raw_stream(w.device)))
+    return packed
 
 
 def dc_fc_quant_layer(x, weights, scales, bias, relu):
@@ -653,7 +668,7 @@ class StackRunner:
                  max_block_ssd=None, dtype=DC_F32, expiry=0, max_rects=1024, device="cuda:0",
                  want_regions=False, pad_input=True, overlap=True, pipeline=True, pack_weights=True,
                  match_method=DC_MATCH_EXHAUSTIVE, k_skip=1, in_place=False, extend_borders=False, device_plan=False,
-                 exact_masks=False, cache_pool_add=False, no_reuse=None, torus=False, want_origins=False):
+                 exact_masks=False, cache_pool_add=False, no_reuse=None, torus=False, want_origins=False, fc_quant=False):
         self.device_plan = bool(device_plan) and not in_place
         self.in_place = bool(in_place)
         self.last_in_place = False
@@ -691,6 +706,8 @@ class StackRunner:
         torch.cuda.set_device(self.device)
         self.w_packed = [None if (w is None or not pack_weights or L["type"] != synth.CONV) else dc_pack_conv_weights(L, w)
                          for L, w in zip(layers, self.w)]
+        if fc_quant:          # fully-connected layers in 8-bit integers
+            self.w_packed = [dc_pack_fc_weights(w) if L["type"] == synth.FC else p for L, w, p in zip(layers, self.w, self.w_packed)]
         self._wpp = (C.c_void_p * nl)(*[None if w is None else w.data_ptr() for w in self.w_packed])
         self._bp = (C.c_void_p * nl)(*[None if b is None else b.data_ptr() for b in self.b])
         self.shapes = synth.tensor_shapes(layers, H, W, self.Ch_tensor)

@@ -672,6 +672,7 @@ int32_t dc_quantize_rows(const void* in, size_t n_rows, size_t K, int32_t dtype,
     if (dtype != DC_F32 && dtype != DC_BF16) return DC_ERR_INVALID_ARG;
     if (n_rows < 1 || K < 1) return DC_ERR_INVALID_ARG;
     if (K > kI8MaxK || n_rows > 0x7fffffffull) return DC_ERR_UNSUPPORTED;
+    if (static_cast<const void*>(q) == in) return DC_ERR_INVALID_ARG;
     DC_TRY_HIP(launch_quantize_rows(in, dtype, n_rows, (int)K, q, scales, as_stream(stream)));
     return DC_OK;
 }
@@ -679,7 +680,7 @@ int32_t dc_quantize_rows(const void* in, size_t n_rows, size_t K, int32_t dtype,
 int32_t dc_fc_quant_workspace_bytes(int32_t n_rows, size_t K, int32_t cout, size_t* bytes) {
     if (!bytes) return DC_ERR_NULL_PTR;
     if (n_rows < 1 || K < 1 || cout < 1) return DC_ERR_INVALID_ARG;
-    if (K > kI8MaxK) return DC_ERR_UNSUPPORTED;
+    if (K > kI8MaxK || n_rows > (1 << 24) || cout > (1 << 20) || ((int64_t)n_rows * cout) >> 34) return DC_ERR_UNSUPPORTED;
     *bytes = fc_i8_workspace(n_rows, (int)K, cout);
     return DC_OK;
 }
@@ -698,6 +699,24 @@ int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* we
     if (reinterpret_cast<uintptr_t>(ws_dev) % 256 || in == out) return DC_ERR_INVALID_ARG;
     DC_TRY_HIP(launch_fc_i8(in, weights, weight_scales, bias, out, n_rows, (int)K, cout, relu, dtype, ws_dev, as_stream(stream)));
     return DC_OK;
+}
+
+int32_t dc_packed_fc_bytes(size_t K, int32_t cout, size_t* bytes) {
+    if (!bytes) return DC_ERR_NULL_PTR;
+    if (K < 1 || cout < 1) return DC_ERR_INVALID_ARG;
+    if (K > kI8MaxK || cout > (1 << 20)) return DC_ERR_UNSUPPORTED;
+    *bytes = packed_fc_scales(K, cout) + (size_t)cout * sizeof(float);
+    return DC_OK;
+}
+
+int32_t dc_pack_fc_weights(const void* weights, size_t K, int32_t cout, int32_t dtype, void* packed, void* stream) {
+    if (!weights || !packed) return DC_ERR_NULL_PTR;
+    size_t bytes = 0;
+    const int rc = dc_packed_fc_bytes(K, cout, &bytes);
+    if (rc) return rc;
+    if (reinterpret_cast<uintptr_t>(packed) % 16) return DC_ERR_INVALID_ARG;
+    return dc_quantize_rows(weights, (size_t)cout, K, dtype, static_cast<int8_t*>(packed),
+                            reinterpret_cast<float*>(static_cast<unsigned char*>(packed) + packed_fc_scales(K, cout)), stream);
 }
 
 int32_t dc_moe_workspace_bytes(const dc_moe* moe, int32_t n_tokens, size_t* bytes) {

@@ -201,9 +201,15 @@ template <typename T, bool TILED>
 hipError_t quantize(const T* x, size_t n_rows, int K, const Rows8& to, float* scales, hipStream_t st) {
     auto go = [&](auto lanes, auto ch) {
         constexpr int LANES = decltype(lanes)::value, CH = decltype(ch)::value, THREADS = LANES > 256 ? LANES : 256;
-        const size_t wgs = (n_rows + THREADS / LANES - 1) / (THREADS / LANES);
-        hipLaunchKernelGGL((quantize_rows_kernel<T, LANES, CH, TILED>), dim3((unsigned)wgs), dim3(THREADS), 0, st, x, n_rows, K, to, scales);
-        return hipGetLastError();
+        constexpr size_t kMost = 1 << 20;            // rows of a launch: its threads are counted in 32 bits
+        for (size_t r = 0; r < n_rows; r += kMost) {
+            const size_t n = std::min(kMost, n_rows - r), wgs = (n + THREADS / LANES - 1) / (THREADS / LANES);
+            hipLaunchKernelGGL((quantize_rows_kernel<T, LANES, CH, TILED>), dim3((unsigned)wgs), dim3(THREADS), 0, st, x + r * K, n, K,
+                               Rows8{to.q + r * to.stride, to.stride, to.width}, scales + r);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
+        return hipSuccess;
     };
     using std::integral_constant;
     const int vecs = (to.width + RowVec<T>::N - 1) / RowVec<T>::N;
@@ -534,26 +540,32 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     }
 }
 
-// A kernel whose LDS is sized at the launch; the attribute is raised once per instantiation.
+// A kernel whose LDS is sized at the launch; the attribute is raised once per instantiation and GPU (a bit each).
 template <typename K>
-hipError_t launch_lds(K kernel, std::atomic<bool>& raised, unsigned wgs, unsigned threads, unsigned lds, const FcI8& P, hipStream_t st) {
-    if (lds > 64 * 1024 && !raised.load()) {
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+hipError_t launch_lds(K kernel, std::atomic<uint64_t>& raised, unsigned wgs, unsigned threads, unsigned lds, const FcI8& P, hipStream_t st) {
+    if (lds > 64 * 1024) {
+        int dev = 0;
+        hipError_t e = hipGetDevice(&dev);
         if (e != hipSuccess) return e;
-        raised.store(true);
+        const uint64_t bit = 1ull << (dev & 63);
+        if (!(raised.load() & bit)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kMaxLds);
+            if (e != hipSuccess) return e;
+            raised.fetch_or(bit);
+        }
     }
     hipLaunchKernelGGL(kernel, dim3(wgs), dim3(threads), lds, st, P);
     return hipGetLastError();
 }
 template <typename T, int NB, int WAVES, int AHEAD, bool OWN>
 hipError_t rows_launch(const FcI8& P, hipStream_t st) {
-    static std::atomic<bool> raised{false};
+    static std::atomic<uint64_t> raised{0};
     const unsigned lds = 256 + (unsigned)std::max(OWN ? P.n_tiles * 64 : 0, WAVES * NB * 1024);
     return launch_lds(fc_i8_rows_kernel<T, NB, WAVES, AHEAD, OWN>, raised, (unsigned)((P.cout + 15) / 16), WAVES * 64, lds, P, st);
 }
 template <typename T, int MT, int NT, int WM, int WN, int STAGES>
 hipError_t gemm(const FcI8& P, hipStream_t st) {
-    static std::atomic<bool> raised{false};
+    static std::atomic<uint64_t> raised{0};
     const size_t wgs = ((size_t)P.n_rows + MT * 16 - 1) / (MT * 16) * (((size_t)P.cout + NT * 16 - 1) / (NT * 16));
     if (wgs > 0x7fffffffu) return hipErrorInvalidValue;
     return launch_lds(fc_i8_gemm_kernel<T, MT, NT, WM, WN, STAGES>, raised, (unsigned)wgs, WM * WN * 64, STAGES * (MT + NT) * 2048, P, st);

@@ -199,6 +199,7 @@ hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, 
 size_t fc_i8_workspace(int n_rows, int K, int cout);
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
                         int dtype, void* ws, hipStream_t st);
+inline size_t packed_fc_scales(size_t K, int cout) { return align_up(K * cout, 16); }      // where they start
 // ---- mixture-of-experts layer (dc_moe.hip) ----
 constexpr int kMoeMaxExperts = 256, kMoeMaxTopK = 16, kMoeMaxTokens = 512;
 size_t moe_workspace(const dc_moe& m, int n_tokens);

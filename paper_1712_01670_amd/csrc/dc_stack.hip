@@ -729,6 +729,7 @@ struct StackCall {
     hipStream_t stage_st[kMaxStages] = {};
     unsigned char *plan_dev = nullptr, *scratch = nullptr;
     size_t area_bytes = 0;
+    unsigned char* stage_scratch(int i) const { return scratch ? scratch + (size_t)(pipe ? P.stage_of(i) : 0) * kConvScratchBytes : nullptr; }      // of layer i
     std::vector<void*> eff;                  // where each tensor of this frame lives
 
     // planned on the GPU
@@ -865,6 +866,15 @@ int StackCall::begin() {
         area_bytes = plans_all / kFramesInFlight / 256 * 256;
         plan_dev = ws_dev + (size_t)area * area_bytes;
         scratch = ws_dev + plans_all / 256 * 256;
+    }
+    for (int i = 0; i < n_layers && packed; ++i) {      // fully-connected layers in 8-bit integers
+        const dc_layer& l = P.layers[i];
+        if (l.type != DC_FC || !packed[i]) continue;
+        const size_t K = (size_t)P.hs[l.in0] * P.ws[l.in0] * P.cs[l.in0];
+        if (K > kI8MaxK) return DC_ERR_UNSUPPORTED;
+        if (reinterpret_cast<uintptr_t>(packed[i]) % 16) return DC_ERR_INVALID_ARG;
+        const size_t need = fc_i8_workspace(n_streams, (int)K, l.cout);
+        if (need && (!scratch || need > kConvScratchBytes || reinterpret_cast<uintptr_t>(scratch) % 16)) return DC_ERR_WORKSPACE;
     }
     devplan = cached && P.device_plan &&
               align_up(P.dl.table_bytes, 256) + P.dl.frame_bytes <= area_bytes && ws_host_bytes >= kDevHostRegion + 256;
@@ -1258,7 +1268,7 @@ int StackCall::emit_layer(int i, hipStream_t st, ConvAdd* add, ConvBatch* batch)
     switch (l.type) {
         case DC_CONV: {
             const int c = P.conv_of[i];
-            unsigned char* const my_scratch = scratch ? scratch + (size_t)(pipe ? P.stage_of(i) : 0) * kConvScratchBytes : nullptr;
+            unsigned char* const my_scratch = stage_scratch(i);
             return run_conv_planned(l, eff[a], weights[i], bias ? bias[i] : nullptr, cached ? tensors_prev[t] : nullptr, eff[t], n_streams,
                                     hs[a], ws[a], dtype, P.tilings[i], cached && !devplan ? &plans[i] : nullptr,
                                     cached && !devplan ? &addrs[i] : nullptr, st, prof, i, n_layers + i,
@@ -1300,6 +1310,13 @@ int StackCall::emit_layer(int i, hipStream_t st, ConvAdd* add, ConvBatch* batch)
             return DC_OK;
         }
         case DC_FC:
+            if (packed && packed[i]) {       // in 8-bit integers
+                const size_t K = (size_t)hs[a] * ws[a] * cs[a];
+                const unsigned char* const block = static_cast<const unsigned char*>(packed[i]);
+                DC_TRY_HIP(launch_fc_i8(eff[a], reinterpret_cast<const int8_t*>(block), reinterpret_cast<const float*>(block + packed_fc_scales(K, l.cout)),
+                                        bias ? bias[i] : nullptr, eff[t], n_streams, (int)K, l.cout, l.relu != 0, dtype, stage_scratch(i), st));
+                return DC_OK;
+            }
             DC_TRY_HIP(launch_fc(eff[a], weights[i], bias ? bias[i] : nullptr, eff[t], n_streams, (size_t)hs[a] * ws[a] * cs[a], l.cout, l.relu, dtype, st));
             return DC_OK;
         case DC_SOFTMAX:

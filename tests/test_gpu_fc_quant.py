@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from paper_1712_01670_amd import binding
+from paper_1712_01670_amd import binding, synth
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -249,3 +249,42 @@ def test_a_head_as_it_is_used(dtype):
     assert err < 0.06, float(err)
     p = binding.dc_softmax_layer(q)
     assert (p.float().sum(-1) - 1).abs().max() < 100 * 2.0 ** -9
+
+
+@pytest.mark.parametrize("mode", ["host", "maps", "replayed", "plain"])
+@pytest.mark.parametrize("dtype", [binding.DC_F32, binding.DC_BF16])
+@pytest.mark.parametrize("n", [1, 3])
+def test_a_stack_whose_head_is_in_8_bits(n, dtype, mode):
+    """StackRunner(fc_quant=True): every frame's fully-connected outputs are dc_fc_quant_layer's of their inputs, bit for bit, the
+    layers in front of them are those of the plain runner, and so is a runner made without it."""
+    layers = synth.alexnet(n_classes=40, width=0.25)
+    H = W = 227
+    ws, bs = synth.he_weights(layers, 5, bias_scale=0.05, input_shape=(H, W, 3))
+    kw = dict(dtype=dtype)
+    if mode in ("maps", "replayed"):
+        kw.update(device_plan=True, exact_masks=True)
+    if mode == "plain":
+        kw.update(overlap=False)
+    runner = binding.StackRunner(layers, ws, bs, n, H, W, 3, fc_quant=True, **kw)
+    plain = binding.StackRunner(layers, ws, bs, n, H, W, 3, **kw)
+    if mode == "replayed":
+        runner.set_replay(1)
+    blocks = {i: binding.dc_quantize_rows(runner.w[i].reshape(runner.w[i].shape[0], -1)) for i, L in enumerate(layers) if L["type"] == synth.FC}
+    rng = np.random.default_rng(0)
+    base = rng.integers(0, 256, (n, H + 16, W + 16, 3), dtype=np.uint8)
+    frames = [torch.from_numpy(np.ascontiguousarray(base[:, f:f + H, f:f + W])).to(DEV) for f in range(6)]
+    for f in frames * (4 if mode == "replayed" else 1):      # (a recording is replayed when its buffers and plan area come round again)
+        got = runner.step(f)
+        torch.cuda.synchronize()
+        want = plain.step(f)
+        torch.cuda.synchronize()
+        for i, L in enumerate(layers):
+            x, y = got[L["in0"]], got[i + 1]
+            if L["type"] == synth.FC:
+                q, s = blocks[i]
+                assert torch.equal(y.view(n, 1, 1, -1), binding.dc_fc_quant_layer(x, q, s, runner.b[i], bool(L["relu"]))), i
+            elif i < min(blocks):
+                assert torch.equal(y, want[i + 1]), i
+        assert torch.isfinite(got[-1].float()).all()
+    if mode == "replayed":
+        assert runner.overlap_counters().replayed > 0
