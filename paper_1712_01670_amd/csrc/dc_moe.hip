@@ -125,6 +125,41 @@ __device__ __forceinline__ uint16_t to_bf16(float v) { return __builtin_bit_cast
 __device__ __forceinline__ void store(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store(uint16_t* p, float v) { *p = to_bf16(v); }
 
+// A value of every lane put together over the wavefront, the result in all of them: within rows of 16 lanes by DPP (a few cycles a
+// step where a shuffle through LDS takes sixty), the four rows by scalars.  Always the same order.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true); }
+template <typename F>
+__device__ __forceinline__ uint32_t wave_all(uint32_t v, F f) {
+    v = f(v, dpp<0xb1>(v));            // lanes 1 apart, 2 apart, then the halves of a row and the row mirrored
+    v = f(v, dpp<0x4e>(v));
+    v = f(v, dpp<0x141>(v));
+    v = f(v, dpp<0x140>(v));
+    const auto row = [&](int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); };
+    return f(f(row(0), row(16)), f(row(32), row(48)));
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return __uint_as_float(wave_all(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ __forceinline__ float wave_max(float v) {       // (a NaN loses)
+    return __uint_as_float(wave_all(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+    return wave_all(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+// Sums over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v) {
+    auto add = [&](auto ctrl, auto rows) { v += __builtin_amdgcn_update_dpp(0, v, decltype(ctrl)::value, decltype(rows)::value, 0xf, false); };
+    using std::integral_constant;
+    add(integral_constant<int, 0x111>(), integral_constant<int, 0xf>());       // lanes before in the row
+    add(integral_constant<int, 0x112>(), integral_constant<int, 0xf>());
+    add(integral_constant<int, 0x114>(), integral_constant<int, 0xf>());
+    add(integral_constant<int, 0x118>(), integral_constant<int, 0xf>());
+    add(integral_constant<int, 0x142>(), integral_constant<int, 0xa>());       // the row before, for the second and the fourth
+    add(integral_constant<int, 0x143>(), integral_constant<int, 0xc>());       // the first two, for the last two
+    return v;
+}
+
 // ---- the choice ---------------------------------------------------------------------------------------------------------
 // Order of the logits as whole numbers: a NaN stands below every number, -inf is 0 and never chosen.
 __device__ __forceinline__ uint32_t logit_key(float l) {
@@ -182,8 +217,7 @@ __device__ __forceinline__ void router_logits(const Moe& P, int token, int e0, f
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) sum[i] += __shfl_xor(sum[i], d);
+        sum[i] = wave_sum(sum[i]);
         if (lane == 0 && e0 + i * STEP < P.experts) logits[e0 + i * STEP] = sum[i] + bias[i];
     }
 }
@@ -199,32 +233,28 @@ __device__ __forceinline__ void choose_experts(const Moe& P, const float* logits
         key[i] = e < P.experts ? logit_key(logits[e]) : 0;
         if (e < P.experts) top = fmaxf(top, logits[e]);
     }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    top = wave_max(top);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
         const int e = i * 64 + lane;
         if (e < P.experts && logits[e] != -INFINITY) sum += expf(logits[e] - top);
     }
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    sum = wave_sum(sum);
     float chosen = 0.f;
     expert = -1;
     gate = 0.f;
     for (int j = 0; j < P.top_k; ++j) {
-        unsigned long long best = 0;
+        uint32_t best = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) best = max(best, key[i]);
+        best = wave_umax(best);
+        if (best == 0) break;
+        int e = -1;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const unsigned long long c = (unsigned long long)key[i] << 32 | (uint32_t)~(i * 64 + lane);      // equal: the lowest index
-            if (key[i] && c > best) best = c;
+            const unsigned long long hit = __ballot(key[i] == best);
+            if (e < 0 && hit) e = i * 64 + __ffsll(hit) - 1;       // equal: the lowest index
         }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) {
-            const unsigned long long o = __shfl_xor(best, d);
-            best = o > best ? o : best;
-        }
-        if (best == 0) break;
-        const int e = (int)~(uint32_t)best;
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i * 64 + lane == e) key[i] = 0;
@@ -313,12 +343,7 @@ __device__ __forceinline__ Part find_part(const Moe& P, const Chosen& C, int a) 
     int parts = 0, blocks = 0;                 // of the experts before
     for (int i = 0; i * 64 < P.experts; ++i) {
         const int n = C.count[i * 64 + lane], own = (n + kMoePart - 1) / kMoePart << 16 | (n + 15) / 16;
-        int sum = own;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
-        }
+        const int sum = wave_scan(own);
         const int before = parts + ((sum - own) >> 16);
         const unsigned long long hit = __ballot(a >= before && a < before + (own >> 16));
         if (hit) {
