@@ -478,14 +478,16 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     }
     if (e < 0) return;
     // Addresses are a uniform base and 32 bits a lane, so that what is ahead costs no registers but its own.  Tile r: half r / CT,
-    // channels 16 (r % CT) on; past the end the last channel again.
+    // channels 16 (r % CT) on; past the end the last channel again (also where a tile starts there: hidden values are made up to
+    // whole pieces).
+    const int row0 = min(o0, channels - 1);
     const unsigned char* wbase[HALVES];
     uint32_t wat[CT];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h)
-        wbase[h] = reinterpret_cast<const unsigned char*>(static_cast<const W*>(DOWN ? P.down : P.up) + (((size_t)e * HALVES + h) * channels + o0) * K);
+        wbase[h] = reinterpret_cast<const unsigned char*>(static_cast<const W*>(DOWN ? P.down : P.up) + (((size_t)e * HALVES + h) * channels + row0) * K);
 #pragma unroll
-    for (int c = 0; c < CT; ++c) wat[c] = (uint32_t)max(0, min(c * 16 + l16, channels - 1 - o0)) * (uint32_t)(K * sizeof(W)) + g * 16;
+    for (int c = 0; c < CT; ++c) wat[c] = (uint32_t)(min(o0 + c * 16 + l16, channels - 1) - row0) * (uint32_t)(K * sizeof(W)) + g * 16;
     const int share = ((whole + 1) / 2 + kMoeWaves - 1) / kMoeWaves * 2, first = wave * share, end = min(whole, first + share);      // this wavefront's pieces
     uintx4 w[4][R];
     auto fetch_w = [&](uintx4 (&to)[R], int p) {
