@@ -519,7 +519,7 @@ int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* we
 /*
  * The same weights in one block, for the fully-connected layers of a stack: int8 [cout][K] and, from the next multiple of 16
  * bytes on, their fp32 scales [cout].  A block passed to dc_run_stack as the packed_weights entry of a DC_FC layer makes the
- * layer run as dc_fc_quant_layer does, with the plain weights unused.
+ * layer run as dc_fc_quant_layer does; its plain weights are not read and their entry may be NULL.
  *   weights dev [cout][K] in `dtype`, packed dev, 16-byte aligned, dc_packed_fc_bytes long
  */
 int32_t dc_packed_fc_bytes(size_t K, int32_t cout, size_t* bytes);
@@ -541,6 +541,7 @@ int32_t dc_pack_fc_weights(const void* weights, size_t K, int32_t cout, int32_t 
  *   router   dev [experts][cin] in `dtype`, router_bias dev fp32 [experts] or NULL
  *   up       dev [experts][hidden][cin], gated: [experts][2][hidden][cin]; down dev [experts][cout][hidden]; both in `wtype`,
  *            which is `dtype` or DC_I8; DC_I8 takes fp32 scales per row: up_scale [experts][(2)][hidden], down_scale [experts][cout]
+ *            (read for DC_I8 alone)
  *   up_bias, down_bias   dev fp32, of the scales' shapes, or NULL
  *   experts_out, gates_out   optional dev int32 / fp32 [n_tokens][top_k]: the choice, in falling order of the logits
  *   ws_dev   dev workspace of at least dc_moe_workspace_bytes, 256-byte aligned; calls that may overlap in time need

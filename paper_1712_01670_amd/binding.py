@@ -582,7 +582,7 @@ def dc_pack_fc_weights(w):
     dc_run_stack takes them."""
     dtype = _rows_dtype("dc_pack_fc_weights", w)
     cout = w.shape[0]
-    K, need = w.numel() // cout, C.c_size_t()
+    K, need = w.numel() // max(cout, 1), C.c_size_t()
     _check("dc_packed_fc_bytes", lib().dc_packed_fc_bytes(K, cout, C.byref(need)))
     with _on(w.device):
         packed = torch.empty(need.value, dtype=torch.uint8, device=w.device)
@@ -623,6 +623,8 @@ def dc_moe_layer(moe, x, router, up, down, router_bias=None, up_bias=None, down_
                               DC_I8 if weights_type == torch.int8 else dtype)
     if weights_type != torch.int8:
         weights_type = x.dtype
+        if up_scale is not None or down_scale is not None:
+            raise ValueError(f"{fn}: scales belong to int8 weights, got {up.dtype}")
     x_shape, router_shape, up_shape, down_shape, gates_shape, bias_shape = shapes
     _want(fn, x, x.dtype, x_shape, dev)
     _want(fn, router, x.dtype, router_shape, dev)

@@ -787,7 +787,7 @@ int StackCall::check() {
     for (int t = 0; t <= n_layers; ++t)
         if (!tensors_cur[t]) return DC_ERR_NULL_PTR;
     for (int i = 0; i < n_layers; ++i)
-        if ((P.layers[i].type == DC_CONV || P.layers[i].type == DC_FC) && !weights[i]) return DC_ERR_NULL_PTR;
+        if ((P.layers[i].type == DC_CONV || (P.layers[i].type == DC_FC && !(packed && packed[i]))) && !weights[i]) return DC_ERR_NULL_PTR;
     if (cached) {
         if (!frames_prev || !tensors_prev || !mv || !best_ssd || !gmv || !n_pass || !block_mask || !ws_dev || !ws_host)
             return DC_ERR_NULL_PTR;

@@ -288,3 +288,29 @@ def test_a_stack_whose_head_is_in_8_bits(n, dtype, mode):
         assert torch.isfinite(got[-1].float()).all()
     if mode == "replayed":
         assert runner.overlap_counters().replayed > 0
+
+
+def test_a_stack_needs_no_plain_weights_behind_a_packed_block():
+    """The plain weights of a layer in 8-bit integers may be gone: NULL entries give the same bits; without a block they are refused."""
+    layers = synth.alexnet(n_classes=24, width=0.25)
+    H = W = 227
+    ws, bs = synth.he_weights(layers, 7, bias_scale=0.05, input_shape=(H, W, 3))
+    frame = torch.randint(0, 256, (2, H, W, 3), dtype=torch.uint8, generator=torch.Generator().manual_seed(3)).to(DEV)
+    fc = [i for i, L in enumerate(layers) if L["type"] == synth.FC]
+    outs = []
+    for gone in (False, True):
+        runner = binding.StackRunner(layers, ws, bs, 2, H, W, 3, fc_quant=True, overlap=False)
+        for i in fc if gone else ():
+            runner._wp[i] = None
+        outs.append(runner.step(frame)[-1].clone())
+        torch.cuda.synchronize()
+    assert fc and torch.equal(*outs)
+    runner = binding.StackRunner(layers, ws, bs, 2, H, W, 3, overlap=False)
+    runner._wp[fc[0]] = None
+    with pytest.raises(binding.DcError):
+        runner.step(frame)
+
+
+def test_a_block_of_no_channels_is_refused():
+    with pytest.raises(binding.DcError):
+        binding.dc_pack_fc_weights(torch.zeros(0, 8, device=DEV))

@@ -302,3 +302,10 @@ def test_features_experts_head_as_they_are_used():
     assert (z.float() - zf).norm() / zf.norm() < 0.1
     p = binding.dc_softmax_layer(z)
     assert (p.float().sum(-1) - 1).abs().max() < 100 * 2.0 ** -9
+
+
+def test_scales_beside_weights_that_have_none_are_refused():
+    c = _case(2, 4, 2, 16, 16, 16, "f32", "f32")
+    c["up_scale"] = torch.ones(4, 32)
+    with pytest.raises(ValueError):
+        _call(c)
