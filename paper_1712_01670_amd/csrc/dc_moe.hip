@@ -360,6 +360,12 @@ __device__ __forceinline__ Part find_part(const Moe& P, const Chosen& C, int a) 
     part.all = parts;
     return part;
 }
+// How many parts there are.
+__device__ __forceinline__ int count_parts(const Moe& P, const Chosen& C) {
+    int parts = 0;
+    for (int i = 0; i * 64 < P.experts; ++i) parts += __builtin_amdgcn_readlane(wave_scan((C.count[i * 64 + (threadIdx.x & 63)] + kMoePart - 1) / kMoePart), 63);
+    return parts;
+}
 // Slots of the part in order, by the first wavefront, a lane per token.
 __device__ __forceinline__ void list_slots(const Moe& P, Chosen& C, const Part& part, int t0, int n_tok) {
     if (threadIdx.x < 64) {
@@ -431,9 +437,10 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
 
 // The product of R tiles of 16 channels of an expert (gated: R / 2 in either half) with a part of its slots: relu or gate of
 // the first layer into the hidden values, or the second layer into the slots' outputs.  The weights are what has to come from
-// memory, once: they go straight into operands (16 rows of 64 bytes an instruction), three pieces of a wavefront
-// ahead, and every wavefront takes a run of K, of whole cache lines; their sums are added through LDS in a fixed
-// order.  The tokens' rows come from L2, a piece ahead, once for R tiles of weights: a row of a fragment costs the CU a look-up for
+// memory, once: they go straight into operands (16 rows of 64 bytes an instruction), two pieces of a wavefront
+// ahead, both halves of a cache line one after the other (reading 268 MB that way takes 51 us, a half of all lines and then the
+// other 62; four rows of 256 bytes 47).  Every wavefront takes a run of K, of whole cache lines; their sums are added through LDS in a
+// fixed order.  The tokens' rows come from L2, once for R tiles of weights: a row of a fragment costs the CU a look-up for
 // every 16 bytes, as a row of weights does, so R is large where there are workgroups enough.  The hidden values lie in the order
 // of the second layer's fragments, 1 KiB a look-up of 16, fp32 or as two bf16 numbers each (the value's rounding and what
 // that leaves), so that the second product sees 16 bits of them: the layer's output is rounded once, as if they were fp32.
@@ -452,7 +459,7 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int l16 = lane & 15, g = lane >> 4;
     const int channels = DOWN ? P.cout : P.hidden, K = DOWN ? P.hidden : P.cin;
-    const int o0 = blockIdx.x * (CT * 16), t0 = blockIdx.z * kMoeTokens, n_tok = min(kMoeTokens, P.n_tokens - t0);
+    const int t0 = blockIdx.z * kMoeTokens, n_tok = min(kMoeTokens, P.n_tokens - t0);
     const int pieces = (K + 4 * PE - 1) / (4 * PE), whole = K / (4 * PE), hidden_pieces = (P.hidden + 4 * PE - 1) / (4 * PE);
     const int piece_bytes = P.block_rows * (V * 64);       // of a block of hidden values
     if constexpr (DOWN || MOST > 1) {
@@ -461,8 +468,17 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
         if (P.route) choose_and_count<T>(P, C, reinterpret_cast<float(*)[kMoeMaxExperts]>(&red[0][0][0]), blockIdx.x == 0 && blockIdx.y == 0);
         else count_experts(P, C, t0, n_tok);
     }
-    const Part part = find_part(P, C, blockIdx.y);
-    const int e = part.e;
+    int tile = blockIdx.x, at = blockIdx.y;
+    if constexpr (DOWN && MOST > 1) {      // an XCD (workgroup number modulo 8) takes a run of the tiles, so that few of them fetch an expert's hidden values
+        const int all = count_parts(P, C) * gridDim.x, number = blockIdx.y * gridDim.x + blockIdx.x;
+        const int xcd = number & 7, j = number >> 3, per = all >> 3, more = all & 7;
+        if (j >= per + (xcd < more)) return;
+        const int i = xcd * per + min(xcd, more) + j;
+        at = i / gridDim.x;
+        tile = i % gridDim.x;
+    }
+    const Part part = find_part(P, C, at);
+    const int e = part.e, o0 = tile * (CT * 16);
     auto add_up = [&]() {
         for (int i = tid; i < n_tok * (CT * 4); i += kMoeWaves * 64) {
             const int t = i / (CT * 4), c = o0 + i % (CT * 4) * 4;
@@ -490,13 +506,17 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     for (int c = 0; c < CT; ++c) wat[c] = (uint32_t)(min(o0 + c * 16 + l16, channels - 1) - row0) * (uint32_t)(K * sizeof(W)) + g * 16;
     const int share = ((whole + 1) / 2 + kMoeWaves - 1) / kMoeWaves * 2, first = wave * share, end = min(whole, first + share);      // this wavefront's pieces
     uintx4 w[4][R];
-    auto fetch_w = [&](uintx4 (&to)[R], int p) {
-        if (p < end)
+    auto fetch_w = [&](int d, int p) {                     // two pieces: a cache line of every row
+        if (p < end) {
+            const uint32_t at = p * 64, at1 = p + 1 < end ? at + 64 : at;
 #pragma unroll
-            for (int r = 0; r < R; ++r) to[r] = load16(wbase[r / CT] + (uint32_t)(p * 64) + wat[r % CT]);
+            for (int r = 0; r < R; ++r) {
+                w[d][r] = load16(wbase[r / CT] + at + wat[r % CT]);
+                w[d + 1][r] = load16(wbase[r / CT] + at1 + wat[r % CT]);
+            }
+        }
     };
-#pragma unroll
-    for (int d = 0; d < 3; ++d) fetch_w(w[d], first + d);
+    fetch_w(0, first);
     floatx4 scale[HALVES], bias[HALVES];                   // of the channels that this wavefront finishes
 #pragma unroll
     for (int h = 0; h < HALVES; ++h)
@@ -527,7 +547,7 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
 #pragma unroll
             for (int j = 0; j < NB; ++j) xat[j] = (uint32_t)(C.slot[min(j * 16 + l16, n - 1)] / P.top_k) * (uint32_t)(P.cin * sizeof(T));
         }
-        constexpr int XRING = MOST == 1 ? 4 : 2, XAHEAD = XRING / 2;       // rows of few tokens are small enough for two pieces ahead
+        constexpr int XRING = NB == 1 ? 4 : 2;             // rows of one block travel by pairs of pieces, too, of two a piece ahead
         Op x[XRING][NB], low[XRING][TWO ? NB : 1];
         auto fetch_x = [&](int b, int p, bool end = false, int k0 = 0) {
 #pragma unroll
@@ -565,14 +585,17 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                 }
             }
         };
+        auto fetch_xs = [&](int d, int p) {                // XRING / 2 pieces
 #pragma unroll
-        for (int d = 0; d < XAHEAD; ++d)
-            if (first + d < end) fetch_x(d, first + d);
+            for (int i = 0; i < XRING / 2; ++i)
+                if (p + i < end) fetch_x((d + i) % XRING, p + i);
+        };
+        fetch_xs(0, first);
         for (int p = first; p < end; p += 4) {
 #pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                if (p + d + XAHEAD < end) fetch_x((d + XAHEAD) % XRING, p + d + XAHEAD);       // (loads come back in order: the rows
-                fetch_w(w[(d + 3) & 3], p + d + 3);                                            // before the weights further ahead)
+            for (int d = 0; d < 4; ++d) {                  // (loads come back in order: the rows before the weights further ahead)
+                if (XRING == 2 || d % 2 == 0) fetch_xs(d + XRING / 2, p + d + XRING / 2);
+                if (d % 2 == 0) fetch_w((d + 2) & 3, p + d + 2);
                 __builtin_amdgcn_sched_barrier(0);
                 if (p + d < end) multiply(w[d], d % XRING);
                 __builtin_amdgcn_sched_barrier(0);
