@@ -112,7 +112,8 @@ struct RowScale {
 
 // Where a row's bytes go: [n_rows][stride], `width` of them (zeros behind K); or tiles of 16 rows x 64 bytes in the order of a
 // fragment's lanes (lane l: row l % 16, bytes 16 (l / 16) on), 1 KiB in one piece, tile (i, j) being number i * n_tiles + j.
-struct Rows8 { int8_t* q; size_t stride; int width; };
+// The counters that the product behind it wants at zero come along.
+struct Rows8 { int8_t* q; size_t stride; int width; int32_t* zero = nullptr; int zeros = 0; };
 __device__ __forceinline__ size_t tile_offset(size_t row, int k0, int n_tiles) {
     return ((row >> 4) * n_tiles + (k0 >> 6)) * 1024 + ((k0 >> 4) & 3) * 256 + (row & 15) * 16 + (k0 & 15);
 }
@@ -142,6 +143,8 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void quantize_rows_kerne
     const int tid = threadIdx.x, part = tid % LANES;
     const size_t row = (size_t)blockIdx.x * ROWS + tid / LANES;
     const bool live = row < n_rows;
+    if (blockIdx.x == 0)
+        for (int i = tid; i < to.zeros; i += THREADS) to.zero[i] = 0;
     const T* const xr = x + (live ? row : 0) * K;
     const int vecs = live ? (to.width + N - 1) / N : 0;
     float f[CH ? CH : 1][N];
@@ -205,7 +208,7 @@ hipError_t quantize(const T* x, size_t n_rows, int K, const Rows8& to, float* sc
         for (size_t r = 0; r < n_rows; r += kMost) {
             const size_t n = std::min(kMost, n_rows - r), wgs = (n + THREADS / LANES - 1) / (THREADS / LANES);
             hipLaunchKernelGGL((quantize_rows_kernel<T, LANES, CH, TILED>), dim3((unsigned)wgs), dim3(THREADS), 0, st, x + r * K, n, K,
-                               Rows8{to.q + r * to.stride, to.stride, to.width}, scales + r);
+                               Rows8{to.q + r * to.stride, to.stride, to.width, to.zero, to.zeros}, scales + r);
             const hipError_t e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
@@ -242,6 +245,9 @@ struct FcI8 {
     const float* bias;
     void* out;
     int n_rows, K, n_tiles, cout, relu;
+    int splits;                // workgroups that share a tile's K, and what they need: sums and counters
+    int* part;                 // [tiles][splits][a tile's sums]
+    int32_t* done;             // [tiles]
 };
 
 template <typename T>
@@ -405,12 +411,14 @@ __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
 // stage is multiplied while the fragments of the next half are read into the other set of registers; one barrier a stage.
 // Rows are whole 16-byte vectors; what lies behind a row of weights meets zeros of the input row, and what lies behind an
 // operand's end reads as zero.
+// SPLIT: P.splits workgroups share a tile, each with a run of K, and the one that comes last adds their integer sums up; nothing
+// waits for another.  The sums go past the XCDs' caches (atomic operations of the GPU's scope).
 constexpr int kBufferFlags = 0x00020000;
 constexpr int kMaxLds = 160 * 1024;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() { __builtin_amdgcn_s_waitcnt(0x0f70 | (N & 15) | (N >> 4) << 14); }
-template <typename T, int MT, int NT, int WM, int WN, int STAGES>
+template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool SPLIT>
 __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     constexpr int WAVES = WM * WN, XI = 2 * MT / WAVES, WI = 2 * NT / WAVES, UM = MT / WM, UN = NT / WN;
     static_assert(2 * MT % WAVES == 0 && 2 * NT % WAVES == 0, "every wavefront loads as many rows of either operand");
@@ -420,10 +428,14 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     const int l16 = lane & 15, g = lane >> 4, wm = wave % WM, wn = wave / WM;
     // workgroup -> tile: every XCD (workgroup number modulo 8) takes a run of the tiles, which go down columns of 8 row tiles
     const int n_m = (P.n_rows + MT * 16 - 1) / (MT * 16), n_n = (P.cout + NT * 16 - 1) / (NT * 16);
-    int tm, tn;
+    int tm, tn, tile = 0, run = 0;
     {
-        const int n = n_m * n_n, xcd = blockIdx.x & 7, j = blockIdx.x >> 3, per = n >> 3, more = n & 7;
-        const int at = xcd * per + min(xcd, more) + j;
+        const int n = n_m * n_n * (SPLIT ? P.splits : 1), xcd = blockIdx.x & 7, j = blockIdx.x >> 3, per = n >> 3, more = n & 7;
+        int at = xcd * per + min(xcd, more) + j;
+        if constexpr (SPLIT) {
+            run = at % P.splits;
+            at = tile = at / P.splits;
+        }
         const int band = at / (8 * n_n), left = min(8, n_m - band * 8), in = at - band * 8 * n_n;
         tm = band * 8 + in % left;
         tn = in / left;
@@ -435,7 +447,8 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     const __amdgpu_buffer_rsrc_t w_rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(P.w) + o0 * P.w_stride, 0,
                                                                             (uint32_t)(chans * P.w_stride), kBufferFlags);
     uint32_t xo[XI], wo[WI];
-    const int r = lane >> 3, v16 = ((lane & 7) ^ r) << 4;
+    const int first = SPLIT ? P.n_tiles / 2 * run / P.splits : 0, stages = (SPLIT ? P.n_tiles / 2 * (run + 1) / P.splits : P.n_tiles / 2) - first;
+    const int r = lane >> 3, v16 = first * 128 + (((lane & 7) ^ r) << 4);
 #pragma unroll
     for (int i = 0; i < XI; ++i) xo[i] = (uint32_t)(((i * WAVES + wave) * 8 + r) * P.x_stride) + v16;
 #pragma unroll
@@ -493,7 +506,6 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     asm volatile("s_barrier" ::: "memory");
     fragments(0, 0);
     int buf = 0;
-    const int stages = P.n_tiles / 2;
     for (int t = 0; t < stages; ++t) {
         const int next = buf + 1 == STAGES ? 0 : buf + 1;
         fragments(1, buf);
@@ -510,6 +522,35 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
         buf = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");       // the loads behind the last stage end before the workgroup does
+    if constexpr (SPLIT) {
+        constexpr int SUMS = UM * UN, THREADS = WAVES * 64;
+        auto sum_at = [&](int who, int i) { return reinterpret_cast<unsigned long long*>(P.part) + ((((size_t)tile * P.splits + who) * SUMS + i) * THREADS + tid) * 2; };
+#pragma unroll
+        for (int i = 0; i < SUMS; ++i) {
+            unsigned long long u[2];
+            __builtin_memcpy(u, &acc[i / UN][i % UN], 16);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) __hip_atomic_store(sum_at(run, i) + h, u[h], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wavefront's sums have arrived
+        __syncthreads();
+        int* const last = reinterpret_cast<int*>(smem);
+        if (tid == 0) *last = __hip_atomic_fetch_add(P.done + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == P.splits - 1;
+        __syncthreads();
+        if (!*last) return;
+        for (int d = 1; d < P.splits; ++d) {
+            const int who = run + d < P.splits ? run + d : run + d - P.splits;
+#pragma unroll
+            for (int i = 0; i < SUMS; ++i) {
+                unsigned long long u[2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) u[h] = __hip_atomic_load(sum_at(who, i) + h, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                intx4 v;
+                __builtin_memcpy(&v, u, 16);
+                acc[i / UN][i % UN] += v;
+            }
+        }
+    }
     const bool vec = P.cout % 4 == 0 && reinterpret_cast<uintptr_t>(P.out) % (4 * sizeof(T)) == 0;
 #pragma unroll
     for (int j = 0; j < UN; ++j) {
@@ -563,12 +604,12 @@ hipError_t rows_launch(const FcI8& P, hipStream_t st) {
     const unsigned lds = 256 + (unsigned)std::max(OWN ? P.n_tiles * 64 : 0, WAVES * NB * 1024);
     return launch_lds(fc_i8_rows_kernel<T, NB, WAVES, AHEAD, OWN>, raised, (unsigned)((P.cout + 15) / 16), WAVES * 64, lds, P, st);
 }
-template <typename T, int MT, int NT, int WM, int WN, int STAGES>
+template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool SPLIT = false>
 hipError_t gemm(const FcI8& P, hipStream_t st) {
     static std::atomic<uint64_t> raised{0};
-    const size_t wgs = ((size_t)P.n_rows + MT * 16 - 1) / (MT * 16) * (((size_t)P.cout + NT * 16 - 1) / (NT * 16));
+    const size_t wgs = ((size_t)P.n_rows + MT * 16 - 1) / (MT * 16) * (((size_t)P.cout + NT * 16 - 1) / (NT * 16)) * (SPLIT ? P.splits : 1);
     if (wgs > 0x7fffffffu) return hipErrorInvalidValue;
-    return launch_lds(fc_i8_gemm_kernel<T, MT, NT, WM, WN, STAGES>, raised, (unsigned)wgs, WM * WN * 64, STAGES * (MT + NT) * 2048, P, st);
+    return launch_lds(fc_i8_gemm_kernel<T, MT, NT, WM, WN, STAGES, SPLIT>, raised, (unsigned)wgs, WM * WN * 64, STAGES * (MT + NT) * 2048, P, st);
 }
 
 // [cout][K] -> rows of whole vectors, zeros behind K
@@ -591,6 +632,7 @@ hipError_t product_few(const FcI8& P, hipStream_t st) {
 // rows 6.7 with 128 x 64, 8.4 with 128 x 128, 7.3 with 64 x 64.
 template <typename T>
 hipError_t product_many(const FcI8& P, hipStream_t st) {
+    if (P.splits > 1) return gemm<T, 4, 4, 2, 4, 4, true>(P, st);
     const long tiles = ((long)P.n_rows + 127) / 128 * ((P.cout + 127) / 128), big = ((long)P.n_rows + 255) / 256 * ((P.cout + 255) / 256);
     if (P.cout <= 64 && tiles > 64) return gemm<T, 8, 4, 2, 4, 2>(P, st);
     if (big >= 768) return gemm<T, 16, 16, 2, 4, 2>(P, st);
@@ -607,16 +649,30 @@ hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, 
                             : quantize<float, false>((const float*)x, n_rows, K, to, scales, st);
 }
 
-// The workspace: the rows in 8 bits, K padded with zeros to whole steps, their scales, and room for weights whose rows are not
-// whole vectors.
-struct I8Space { size_t scales, weights, end; };
+// Workgroups that share a tile of 64 x 64: as many as give every CU one, with eight stages of K each at least.  Putting the sums together
+// costs 2.5 us, so K has to be long: with more than 64 rows (us, alone -> shared) 2048 -> 1000 on 128 rows 10.4 -> 10.7, 4096 -> 1024
+// 14.7 -> 13.4, 9216 -> 4096 30.5 -> 24.9, 25088 -> 512 50.1 -> 28.9; where the other side is the kernel of few rows 4096 -> 4096 on 64
+// rows 14.8 -> 15.5, 9216 -> 4096 23.7 -> 20.7, 25088 -> 512 36.8 -> 27.6, on 17 rows 13.3 -> 15.1, 18.4 -> 18.6, 28.0 -> 25.1.
+static long i8_tiles(int n_rows, int cout) { return ((long)n_rows + 63) / 64 * (((long)cout + 63) / 64); }
+static int i8_splits(int n_rows, int K, int cout) {
+    const int stages = (K + 127) / 128;
+    if (n_rows <= 16 || stages < (n_rows <= kI8FewRows ? 64 : 32)) return 1;
+    return (int)std::max(1l, std::min(256 / i8_tiles(n_rows, cout), (long)stages / 8));
+}
+
+// The workspace: the rows in 8 bits, K padded with zeros to whole steps, their scales, room for weights whose rows are not
+// whole vectors, and the sums and counters of tiles that workgroups share.
+struct I8Space { size_t scales, weights, part, done, end; };
 static I8Space i8_space(int n_rows, int K, int cout) {
-    if (n_rows == 1) return I8Space{0, 0, 0};
+    if (n_rows == 1) return I8Space{0, 0, 0, 0, 0};
     const size_t row = align_up(K, 128);
     I8Space s;
     s.scales = align_up(align_up(n_rows, 16) * row, 256);
     s.weights = s.scales + align_up((size_t)n_rows * sizeof(float), 256);
-    s.end = s.weights + (n_rows > kI8FewRows ? align_up(cout * row, 256) : 0);
+    s.part = s.weights + (n_rows > kI8FewRows ? align_up(cout * row, 256) : 0);
+    const int splits = i8_splits(n_rows, K, cout);
+    s.done = s.part + (splits > 1 ? i8_tiles(n_rows, cout) * splits * (64 * 64 * sizeof(int)) : 0);
+    s.end = s.done + (splits > 1 ? align_up(i8_tiles(n_rows, cout) * sizeof(int32_t), 256) : 0);
     return s;
 }
 size_t fc_i8_workspace(int n_rows, int K, int cout) { return i8_space(n_rows, K, cout).end; }
@@ -628,13 +684,22 @@ static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
     const int width = (int)align_up(P.K, 128);
     P.x = x; P.n_tiles = width / 64; P.w_stride = P.K;
     if (P.n_rows == 1) return rows_launch<T, 1, 16, 2, true>(P, st);
-    const bool few = P.n_rows <= kI8FewRows;
-    const Rows8 to{ws, (size_t)width, width};
+    const bool vectors = P.K % 16 == 0 && reinterpret_cast<uintptr_t>(P.w) % 16 == 0;
+    P.splits = i8_splits(P.n_rows, P.K, P.cout);
+    // (the GEMM wants whole vectors: weights of another form are copied for many rows, and few rows have their own kernel)
+    const bool few = P.n_rows <= kI8FewRows && !(P.splits > 1 && vectors);
+    Rows8 to{ws, (size_t)width, width};
+    if (!few && P.splits > 1) {
+        P.part = reinterpret_cast<int*>(ws + space.part);
+        P.done = reinterpret_cast<int32_t*>(ws + space.done);
+        to.zero = P.done;
+        to.zeros = (int)i8_tiles(P.n_rows, P.cout);
+    }
     P.xq = ws; P.x_stride = width; P.sx = sx;
     hipError_t e = few ? quantize<T, true>(x, P.n_rows, P.K, to, sx, st) : quantize<T, false>(x, P.n_rows, P.K, to, sx, st);
     if (e != hipSuccess) return e;
     if (few) return product_few<T>(P, st);
-    if (P.K % 16 || reinterpret_cast<uintptr_t>(P.w) % 16) {
+    if (!vectors) {
         int8_t* const w = ws + space.weights;
         for (int c = 0; c < P.cout; c += 65535) {
             const int n = std::min(65535, P.cout - c);

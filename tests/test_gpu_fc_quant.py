@@ -314,3 +314,54 @@ def test_a_stack_needs_no_plain_weights_behind_a_packed_block():
 def test_a_block_of_no_channels_is_refused():
     with pytest.raises(binding.DcError):
         binding.dc_pack_fc_weights(torch.zeros(0, 8, device=DEV))
+
+
+LONG = [(17, 8208, 65), (33, 131072, 20), (64, 9216, 1000), (65, 4096, 1), (66, 4101, 70), (130, 4112, 100), (250, 8191, 64), (1000, 5000, 64)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", LONG)
+def test_long_rows_shared_by_workgroups(shape, dtype):
+    """Tiles whose K several workgroups share: as the definition, the same bits call after call in one workspace, and those of single rows."""
+    n, k, cout = shape
+    x = _rows(n, k, dtype, n, "relu")
+    w, s, b = _weights(cout, k, n)
+    dev = [t.to(DEV) for t in (x, w, s, b)]
+    got = binding.dc_fc_quant_layer(*dev, True)
+    want = _expected(x, w, s, b, True)
+    q, sc = _quantized(x)
+    terms = np.abs((q @ w.double().numpy().T) * sc.astype(np.float64)[:, None] * s.double().numpy()) + b.double().abs().numpy()
+    _check(got, want, dtype, terms)
+    for _ in range(5):
+        assert torch.equal(binding.dc_fc_quant_layer(*dev, True), got)
+    for r in (0, n - 1):
+        assert torch.equal(binding.dc_fc_quant_layer(dev[0][r:r + 1].contiguous(), *dev[1:], True)[0], got[r])
+
+
+def test_long_rows_on_two_streams_and_in_graphs():
+    """Workspaces and counters of calls that overlap are their own; a replayed graph clears its counters each time."""
+    k, cout = 8192, 300
+    w, s, b = (t.to(DEV) for t in _weights(cout, k, 4))
+    xs = [_rows(n, k, torch.bfloat16, n).to(DEV) for n in (40, 150)]
+    want = [binding.dc_fc_quant_layer(x, w, s, b, False) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    got = [[], []]
+    for _ in range(10):
+        for i, st in enumerate(streams):
+            with torch.cuda.stream(st):
+                got[i].append(binding.dc_fc_quant_layer(xs[i], w, s, b, False))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, want[i]) for i in range(2) for g in got[i])
+    static = torch.zeros_like(xs[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = binding.dc_fc_quant_layer(static, w, s, b, False)
+    for rep in range(4):
+        static.copy_(xs[1] if rep % 2 == 0 else -xs[1])
+        g.replay()
+        eager = binding.dc_fc_quant_layer(xs[0], w, s, b, False)
+        torch.cuda.synchronize()
+        assert torch.equal(eager, want[0])
+        assert torch.equal(out, binding.dc_fc_quant_layer(xs[1] if rep % 2 == 0 else -xs[1], w, s, b, False))
+    assert torch.equal(binding.dc_fc_quant_layer(xs[1], w, s, b, False), want[1])
