@@ -135,7 +135,9 @@ __device__ __forceinline__ void store8(const Rows8& to, size_t row, int k0, cons
 }
 
 // LANES threads share a row, a vector each and LANES vectors further the next.  CH > 0: they hold the row in registers, so it is
-// read once; CH == 0: a row that is too long for that is read twice, the second time from the cache.
+// read once; CH == 0: a row that is too long for that is read twice, the second time from the cache.  Memory bounds it where there are many
+// rows: 16384 x 4096 bf16 46.7 us (201 MB, 4.3 TB/s), 12544 x 1024 14.6 us from memory, 7.9 from the cache; 3 to 5 us, the way
+// through the row's maximum, where there are few.
 template <typename T, int LANES, int CH, bool TILED>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void quantize_rows_kernel(const T* __restrict__ x, size_t n_rows, int K, Rows8 to,
                                                                                   float* __restrict__ scales) {
@@ -277,7 +279,9 @@ constexpr int kI8FewRows = 64;
 // their integer sums through LDS.  The weights are what has to come from memory: they go straight from there into fragments
 // (16 rows of 64 bytes an instruction), AHEAD steps of a wavefront before they are multiplied.  The rows come from L2, in tiles.
 // OWN: there is one row, and every workgroup rounds it itself, into LDS, while its first weights travel, which saves a launch
-// (9216 -> 4096: 9.3 us against 8.6 + 3.1; four rows that way 15.0 against 8.6 + 3.1).
+// (9216 -> 4096: 9.3 us against 8.6 + 3.1; four rows that way 15.0 against 8.6 + 3.1).  What bounds it: one row 9216 -> 4096 fp32
+// 10.2 us, 3.7 TB/s of weights, of which 2 us are the start of the kernel and the rounding; small layers the way to memory and back, 1152 -> 100
+// 5.4 us; 64 rows (14.0 us, 9216 -> 4096) their 590 KB a CU from L2 and a look-up for every 16 bytes of weights.
 template <typename T, int NB, int WAVES, int AHEAD, bool OWN>
 __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
     static_assert(!OWN || NB == 1, "");
@@ -410,7 +414,9 @@ __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
 // row r are stored in the order v ^ (r % 8), so that eight neighbouring lanes of a fragment ask 128 different bytes.  Half a
 // stage is multiplied while the fragments of the next half are read into the other set of registers; one barrier a stage.
 // Rows are whole 16-byte vectors; what lies behind a row of weights meets zeros of the input row, and what lies behind an
-// operand's end reads as zero.
+// operand's end reads as zero.  The matrix instructions bound it: 4096 -> 4096 on 16384 rows 295 to 303 us, 1.85 POP/s, where the same
+// instructions without any load reach 2.26 (the power limit, with random numbers) and a library's product of 8192 x 8192 x 8192
+// 2.04; 1024 -> 256 on 12544 rows (196 tiles, one a CU) 11.3 us, mostly the first and the last stage.
 // SPLIT: P.splits workgroups share a tile, each with a run of K, and the one that comes last adds their integer sums up; nothing
 // waits for another.  The sums go past the XCDs' caches (atomic operations of the GPU's scope).
 constexpr int kBufferFlags = 0x00020000;

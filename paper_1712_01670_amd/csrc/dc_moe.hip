@@ -265,7 +265,8 @@ __device__ __forceinline__ void choose_experts(const Moe& P, const float* logits
     if (expert >= 0 && P.renormalize) gate /= chosen;
 }
 
-// A workgroup takes a token: its wavefronts deal the experts among themselves, the first one chooses.
+// A workgroup takes a token: its wavefronts deal the experts among themselves, the first one chooses.  Latency bounds it, a trip to memory,
+// one to L2 and the sums over a wavefront: 64 tokens of 2048 bf16, 32 experts 6.4 us, 16 of 1024 fp32, 8 experts 4.4 us.
 constexpr int kRouterWaves = 16;
 template <typename T>
 __global__ __launch_bounds__(kRouterWaves * 64) void moe_choose_kernel(Moe P) {
@@ -429,6 +430,8 @@ __device__ __forceinline__ void combine(const Moe& P, const int* choice, int tok
     for (int q = 0; q < 4; ++q)
         if (c + q < P.cout) store(out + q, sum[q]);
 }
+// More than 16 tokens: a launch of its own (64 tokens x 4 choices of 2048 4.7 us, of which 2.7 are any launch's; as part of the second layers
+// it would take an atomic per workgroup and token group).
 template <typename T>
 __global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
     const int c = (blockIdx.x * 256 + threadIdx.x) * 4, token = blockIdx.y;
@@ -444,6 +447,10 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(Moe P) {
 // every 16 bytes, as a row of weights does, so R is large where there are workgroups enough.  The hidden values lie in the order
 // of the second layer's fragments, 1 KiB a look-up of 16, fp32 or as two bf16 numbers each (the value's rounding and what
 // that leaves), so that the second product sees 16 bits of them: the layer's output is rounded once, as if they were fp32.
+// Measured, first and second layers (rate of the weights): 64 tokens, 32 experts, 4 of 2048 -> 2 x 1024 -> 2048 bf16 51 us (5.2 TB/s)
+// and 29 (4.6); 8 experts, 2 of 4096 -> 2 x 8192 -> 4096 in 8 bits 113 (4.7) and 73 (3.7: the hidden values, twice 16 bits, are four times
+// a row of weights); 16 tokens, 8 experts, 2 of 1024 -> 2048 -> 1024 fp32 17 and 17 (4.0); one token, 2 of 2048 -> 2 x 4096 -> 2048 bf16 17
+// (3.9) and 13 (2.5): 5 us of each are the start of the kernel, the first trip to memory and the sums' way out.
 __device__ __forceinline__ int opaque(int v) {      // a value the optimiser computes nothing from ahead of time
     asm volatile("" : "+v"(v));
     return v;
