@@ -705,7 +705,9 @@ static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
     hipError_t e = few ? quantize<T, true>(x, P.n_rows, P.K, to, sx, st) : quantize<T, false>(x, P.n_rows, P.K, to, sx, st);
     if (e != hipSuccess) return e;
     if (few) return product_few<T>(P, st);
-    if (!vectors) {
+    // Rows that begin inside a cache line cost more lines a stage: from 2.5e10 products on padded copies of the weights pay (us, as they are ->
+    // copied: 2064 -> 2048 on 6272 rows 65.0 -> 61.3, 4112 -> 1024 on 12544 123 -> 111; 2064 -> 2048 on 3136 36.8 -> 38.8, 576 -> 256 on 12544 22.5 -> 24.5).
+    if (!vectors || (P.K % 128 && (double)P.n_rows * P.K * P.cout >= 2.5e10)) {
         int8_t* const w = ws + space.weights;
         for (int c = 0; c < P.cout; c += 65535) {
             const int n = std::min(65535, P.cout - c);

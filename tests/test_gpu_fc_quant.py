@@ -365,3 +365,14 @@ def test_long_rows_on_two_streams_and_in_graphs():
         assert torch.equal(eager, want[0])
         assert torch.equal(out, binding.dc_fc_quant_layer(xs[1] if rep % 2 == 0 else -xs[1], w, s, b, False))
     assert torch.equal(binding.dc_fc_quant_layer(xs[1], w, s, b, False), want[1])
+
+
+@pytest.mark.parametrize("shape", [(6300, 2064, 2000), (6300, 2060, 2000), (4100, 2064, 2000)])
+def test_large_products_of_any_row_length(shape):
+    """Rows of many cache lines that begin inside one: as 64 rows at a time, bit for bit."""
+    n, k, cout = shape
+    x = _rows(n, k, torch.bfloat16, 1).to(DEV)
+    w, s, b = (t.to(DEV) for t in _weights(cout, k, 2))
+    got = binding.dc_fc_quant_layer(x, w, s, b, False)
+    for r in (0, 1000, n - 64):
+        assert torch.equal(got[r:r + 64], binding.dc_fc_quant_layer(x[r:r + 64], w, s, b, False)), r
