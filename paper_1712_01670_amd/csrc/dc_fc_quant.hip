@@ -265,12 +265,29 @@ __device__ __forceinline__ float finish(int sum, float sw, float sx, float bias,
     return relu && v < 0.f ? 0.f : v;
 }
 
-// 16 weights of a row from k0 on; past the row's end zeros.
+// 16 weights of a row from k0 on; past the row's end zeros: what overlaps the end comes from the row's last 16 bytes (one by one it
+// would take 3 us longer, 1023 -> 1000 on 64 rows 12.0).
 __device__ __forceinline__ intx4 weights16(const int8_t* __restrict__ row, int k0, int K) {
     if (k0 + 16 <= K) return *reinterpret_cast<const intx4_any*>(row + k0);
-    intx4 v{0, 0, 0, 0};
-    for (int e = 0; k0 + e < K; ++e) v[e >> 2] |= (int)((uint32_t)(uint8_t)row[k0 + e] << (8 * (e & 3)));
-    return v;
+    unsigned long long lo = 0, hi = 0;
+    if (k0 < K) {
+        if (K >= 16) {
+            const intx4 v = *reinterpret_cast<const intx4_any*>(row + K - 16);
+            const int bits = (k0 - (K - 16)) * 8;          // 8 .. 120
+            lo = (unsigned long long)(uint32_t)v[1] << 32 | (uint32_t)v[0];
+            hi = (unsigned long long)(uint32_t)v[3] << 32 | (uint32_t)v[2];
+            if (bits >= 64) { lo = hi >> (bits - 64); hi = 0; }
+            else { lo = lo >> bits | hi << (64 - bits); hi >>= bits; }
+        } else {
+#pragma unroll 1
+            for (int e = 0; k0 + e < K; ++e) {
+                const unsigned long long u = (uint8_t)row[k0 + e];
+                if (e < 8) lo |= u << (8 * e);
+                else hi |= u << (8 * e - 64);
+            }
+        }
+    }
+    return intx4{(int)(uint32_t)lo, (int)(uint32_t)(lo >> 32), (int)(uint32_t)hi, (int)(uint32_t)(hi >> 32)};
 }
 
 constexpr int kI8FewRows = 64;
