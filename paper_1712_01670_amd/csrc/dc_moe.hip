@@ -46,6 +46,20 @@ __device__ __forceinline__ uintx4 load16(const E* p) {
     __builtin_memcpy(&v, p, 16);
     return v;
 }
+// 16 bytes of a row whose elements begin inside words of 4 bytes: the five words that hold them, put together where they are used
+// (loads at such addresses run at less than half the rate: the layers of 2049 -> 2 x 1025 -> 2049 below took 2.3 times the time of
+// 2048 -> 2 x 1024 -> 2048).  `at` is an address, whose last two bits say where in its word it begins, relative to a base at a word; each
+// word read holds a byte that is asked for.
+__device__ __forceinline__ uintx4 load_words(const unsigned char* base, uint32_t at) {
+    return load16(reinterpret_cast<const uint32_t*>(__builtin_assume_aligned(base + (at & ~3u), 4)));
+}
+__device__ __forceinline__ uint32_t load_word_behind(const unsigned char* base, uint32_t at) {
+    return *reinterpret_cast<const uint32_t*>(base + ((at + 15) & ~3u));
+}
+__device__ __forceinline__ void shift_words(uintx4& v, uint32_t behind, uint32_t at) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbyte(i < 3 ? v[i + 1] : behind, v[i], at);
+}
 // The same from element k0 of a row of K, zeros behind its end: what overlaps the end comes from the row's last 16 bytes.
 template <typename E>
 __device__ __forceinline__ uintx4 load16_end(const E* __restrict__ row, int k0, int K) {
@@ -456,11 +470,12 @@ __device__ __forceinline__ int opaque(int v) {      // a value the optimiser com
     return v;
 }
 enum { kUpRelu = 0, kUpGated = 1, kDown = 2 };
-template <typename T, typename W, int KIND, int R, int MOST>
+template <typename T, typename W, int KIND, int R, int MOST, bool ODD>      // ODD: rows that begin inside words of 4 bytes
 __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     typedef Operand<T, W> Op;
     constexpr int PE = Op::PE, V = Op::V, HALVES = KIND == kUpGated ? 2 : 1, CT = R / HALVES, PLANES = sizeof(T) == 2 ? 2 : 1;
     constexpr bool DOWN = KIND == kDown, TWO = DOWN && PLANES == 2, ADDS = DOWN && MOST == 1;      // ADDS: the slots' outputs up, too
+    constexpr bool ODD_X = ODD && !DOWN && sizeof(T) == 2;
     __shared__ Chosen C;
     __shared__ floatx4 red[kMoeWaves][R][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -505,21 +520,35 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
     // whole pieces).
     const int row0 = min(o0, channels - 1);
     const unsigned char* wbase[HALVES];
-    uint32_t wat[CT];
+    uint32_t wat[ODD ? R : CT];
 #pragma unroll
-    for (int h = 0; h < HALVES; ++h)
+    for (int h = 0; h < HALVES; ++h) {
         wbase[h] = reinterpret_cast<const unsigned char*>(static_cast<const W*>(DOWN ? P.down : P.up) + (((size_t)e * HALVES + h) * channels + row0) * K);
+        if (ODD || h == 0)
 #pragma unroll
-    for (int c = 0; c < CT; ++c) wat[c] = (uint32_t)(min(o0 + c * 16 + l16, channels - 1) - row0) * (uint32_t)(K * sizeof(W)) + g * 16;
+            for (int c = 0; c < CT; ++c) {
+                wat[h * CT + c] = (uint32_t)(min(o0 + c * 16 + l16, channels - 1) - row0) * (uint32_t)(K * sizeof(W)) + g * 16;
+                if constexpr (ODD) wat[h * CT + c] += reinterpret_cast<uintptr_t>(wbase[h]) & 3;
+            }
+        if constexpr (ODD) wbase[h] -= reinterpret_cast<uintptr_t>(wbase[h]) & 3;
+    }
     const int share = ((whole + 1) / 2 + kMoeWaves - 1) / kMoeWaves * 2, first = wave * share, end = min(whole, first + share);      // this wavefront's pieces
     uintx4 w[4][R];
+    uint32_t w_behind[4][ODD ? R : 1];
     auto fetch_w = [&](int d, int p) {                     // two pieces: a cache line of every row
         if (p < end) {
             const uint32_t at = p * 64, at1 = p + 1 < end ? at + 64 : at;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                w[d][r] = load16(wbase[r / CT] + at + wat[r % CT]);
-                w[d + 1][r] = load16(wbase[r / CT] + at1 + wat[r % CT]);
+                if constexpr (ODD) {
+                    w[d][r] = load_words(wbase[r / CT] + at, wat[r]);
+                    w[d + 1][r] = load_words(wbase[r / CT] + at1, wat[r]);
+                    w_behind[d][r] = load_word_behind(wbase[r / CT] + at, wat[r]);
+                    w_behind[d + 1][r] = load_word_behind(wbase[r / CT] + at1, wat[r]);
+                } else {
+                    w[d][r] = load16(wbase[r / CT] + at + wat[r % CT]);
+                    w[d + 1][r] = load16(wbase[r / CT] + at1 + wat[r % CT]);
+                }
             }
         }
     };
@@ -550,12 +579,14 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
 #pragma unroll
             for (int j = 0; j < NB; ++j) xbase[j] = tiles + (size_t)j * PLANES * hidden_pieces * piece_bytes;
         } else {
-            xbase[0] = static_cast<const unsigned char*>(P.x);
+            const uint32_t into = ODD_X ? reinterpret_cast<uintptr_t>(P.x) & 3 : 0;
+            xbase[0] = static_cast<const unsigned char*>(P.x) - into;
 #pragma unroll
-            for (int j = 0; j < NB; ++j) xat[j] = (uint32_t)(C.slot[min(j * 16 + l16, n - 1)] / P.top_k) * (uint32_t)(P.cin * sizeof(T));
+            for (int j = 0; j < NB; ++j) xat[j] = (uint32_t)(C.slot[min(j * 16 + l16, n - 1)] / P.top_k) * (uint32_t)(P.cin * sizeof(T)) + into;
         }
         constexpr int XRING = NB == 1 ? 4 : 2;             // rows of one block travel by pairs of pieces, too, of two a piece ahead
         Op x[XRING][NB], low[XRING][TWO ? NB : 1];
+        uint32_t x_behind[XRING][ODD_X ? NB : 1];
         auto fetch_x = [&](int b, int p, bool end = false, int k0 = 0) {
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
@@ -568,6 +599,10 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                     }
                 } else if (end) {
                     x[b][j].load_end(reinterpret_cast<const T*>(xbase[0] + xat[j]), k0, K);
+                } else if constexpr (ODD_X) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) x[b][j].v[v] = load_words(xbase[0] + (uint32_t)(p * (V * 64) + v * 16), xat[j] + g * (V * 16));
+                    x_behind[b][j] = load_word_behind(xbase[0] + (uint32_t)(p * (V * 64) + (V - 1) * 16), xat[j] + g * (V * 16));
                 } else {
 #pragma unroll
                     for (int v = 0; v < V; ++v) x[b][j].v[v] = load16(xbase[0] + (uint32_t)(p * (V * 64) + v * 16) + (xat[j] + g * (V * 16)));
@@ -579,11 +614,19 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int j = 0; j < NB; ++j) acc[r][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-        auto multiply = [&](const uintx4 (&weights)[R], int b) {
+        auto multiply = [&](int d, int b, bool end = false) {
+            if constexpr (ODD_X)
+                if (!end)
+#pragma unroll
+                    for (int j = 0; j < NB; ++j)
+#pragma unroll
+                        for (int v = 0; v < V; ++v) shift_words(x[b][j].v[v], v + 1 < V ? x[b][j].v[v + 1 < V ? v + 1 : v][0] : x_behind[b][j], xat[j]);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                uintx4 raw = weights[r];
+                uintx4 raw = w[d][r];
                 asm volatile("" : "+v"(raw));                  // (converted here, not where it is loaded: the ring holds bytes)
+                if constexpr (ODD)
+                    if (!end) shift_words(raw, w_behind[d][r], wat[r]);
                 const Op o(raw);
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
@@ -604,16 +647,16 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                 if (XRING == 2 || d % 2 == 0) fetch_xs(d + XRING / 2, p + d + XRING / 2);
                 if (d % 2 == 0) fetch_w((d + 2) & 3, p + d + 2);
                 __builtin_amdgcn_sched_barrier(0);
-                if (p + d < end) multiply(w[d], d % XRING);
+                if (p + d < end) multiply(d, d % XRING);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (pieces > whole && wave == kMoeWaves - 1) {         // the piece that K ends in
             const int k0 = opaque(whole * (4 * PE) + g * PE);
 #pragma unroll
-            for (int r = 0; r < R; ++r) w[0][r] = load16_end(reinterpret_cast<const W*>(wbase[r / CT] + (wat[r % CT] - g * 16)), k0, K);
+            for (int r = 0; r < R; ++r) w[0][r] = load16_end(reinterpret_cast<const W*>(wbase[r / CT] + (wat[ODD ? r : r % CT] - g * 16)), k0, K);
             fetch_x(0, whole, true, k0);
-            multiply(w[0], 0);
+            multiply(0, 0, true);
         }
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
@@ -672,11 +715,17 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
 }
 
 template <typename T, typename W, int KIND, int R>
-hipError_t expert_launch_as(const Moe& P, unsigned tiles, unsigned parts, hipStream_t st) {
+hipError_t expert_launch_as(const Moe& P, unsigned tiles, unsigned parts, bool odd, hipStream_t st) {
     const dim3 grid(tiles, parts, (unsigned)((P.n_tokens + kMoeTokens - 1) / kMoeTokens)), block(kMoeWaves * 64);
-    if (P.n_tokens <= 16) hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 1>), grid, block, 0, st, P);
-    else hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 2>), grid, block, 0, st, P);
-    return hipGetLastError();
+    auto go = [&](auto is_odd) {
+        constexpr bool ODD = decltype(is_odd)::value;
+        if (P.n_tokens <= 16) hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 1, ODD>), grid, block, 0, st, P);
+        else hipLaunchKernelGGL((moe_expert_kernel<T, W, KIND, R, 2, ODD>), grid, block, 0, st, P);
+        return hipGetLastError();
+    };
+    if constexpr (sizeof(W) < 4)
+        if (odd) return go(std::true_type());
+    return go(std::false_type());
 }
 // Tiles of channels a workgroup: more of them share a fragment of the rows, fewer give more workgroups.  Few tokens have one fragment
 // and want four workgroups a CU (us, four tiles -> fewer: 1024 -> 2048 -> 1024 fp32 16 rows 22.7 + 25.8 -> 20.7 + 22.8), more want the sharing
@@ -692,10 +741,13 @@ Shape shape_of(const Moe& P, int channels, int halves, unsigned parts) {
 }
 template <typename T, typename W, int KIND>
 hipError_t expert_launch(const Moe& P, const Shape& s, unsigned parts, hipStream_t st) {
-    if (s.tiles == 4) return expert_launch_as<T, W, KIND, 4>(P, s.wgs, parts, st);
+    const size_t row = (KIND == kDown ? P.hidden : P.cin) * sizeof(W);
+    bool odd = (reinterpret_cast<uintptr_t>(KIND == kDown ? P.down : P.up) | row) & 3;
+    if (KIND != kDown) odd = odd || ((reinterpret_cast<uintptr_t>(P.x) | P.cin * sizeof(T)) & 3);
+    if (s.tiles == 4) return expert_launch_as<T, W, KIND, 4>(P, s.wgs, parts, odd, st);
     if constexpr (KIND != kUpGated)
-        if (s.tiles == 1) return expert_launch_as<T, W, KIND, 1>(P, s.wgs, parts, st);
-    return expert_launch_as<T, W, KIND, 2>(P, s.wgs, parts, st);
+        if (s.tiles == 1) return expert_launch_as<T, W, KIND, 1>(P, s.wgs, parts, odd, st);
+    return expert_launch_as<T, W, KIND, 2>(P, s.wgs, parts, odd, st);
 }
 
 template <typename T, typename W>
