@@ -299,7 +299,9 @@ constexpr int kI8FewRows = 64;
 // (9216 -> 4096: 9.3 us against 8.6 + 3.1; four rows that way 15.0 against 8.6 + 3.1).  What bounds it: one row 9216 -> 4096 fp32
 // 10.2 us, 3.7 TB/s of weights, of which 2 us are the start of the kernel and the rounding; small layers the way to memory and back, 1152 -> 100
 // 5.4 us; 64 rows (14.0 us, 9216 -> 4096) their 590 KB a CU from L2 and a look-up for every 16 bytes of weights.
-template <typename T, int NB, int WAVES, int AHEAD, bool OWN>
+// ODD: rows of weights that begin inside words of 4 bytes: the five words that hold 16 of them (each holds a byte that is asked for), shifted
+// where they are multiplied (loads at such addresses run at half the rate: 9217 -> 4000, one row, 22.7 us, 9216 -> 4000 12.4).
+template <typename T, int NB, int WAVES, int AHEAD, bool OWN, bool ODD>
 __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
     static_assert(!OWN || NB == 1, "");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
@@ -309,12 +311,24 @@ __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
     // channels past the end repeat the last one (not stored)
     const int8_t* const wrow = P.w + (size_t)min(o0 + l16, P.cout - 1) * P.K;
     const int steps = P.n_tiles / 2, whole = P.K / 128;
-    struct Step { intx4 w[2], x[OWN ? 1 : NB][2]; };
+    struct Step { intx4 w[2], x[OWN ? 1 : NB][2]; int behind[ODD ? 2 : 1]; };
+    typedef int intx4_word __attribute__((ext_vector_type(4), aligned(4)));
+    const uint32_t into = ODD ? reinterpret_cast<uintptr_t>(wrow) & 3 : 0;
+    const int8_t* const words = wrow - into;
+    const int word_behind = into ? 16 : 12;
     const int8_t* const xt = P.xq + lane * 16;
     auto fetch = [&](Step& b, int s) {
         if (s < whole) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) b.w[h] = *reinterpret_cast<const intx4_any*>(wrow + s * 128 + h * 64 + g * 16);
+            for (int h = 0; h < 2; ++h) {
+                const int at = s * 128 + h * 64 + g * 16;
+                if constexpr (ODD) {
+                    b.w[h] = *reinterpret_cast<const intx4_word*>(words + at);
+                    b.behind[h] = *reinterpret_cast<const int*>(words + at + word_behind);
+                } else {
+                    b.w[h] = *reinterpret_cast<const intx4_any*>(wrow + at);
+                }
+            }
         } else if (s < steps) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) b.w[h] = weights16(wrow, s * 128 + h * 64 + g * 16, P.K);
@@ -393,15 +407,21 @@ __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
             fetch(step[(d + AHEAD) % (AHEAD + 1)], s + (d + AHEAD) * WAVES);
             __builtin_amdgcn_sched_barrier(0);
             const Step& b = step[d];
+            const uint32_t by = s + d * WAVES < whole ? into : 0;          // (a row's end comes in its place)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h) {
+                intx4 w = b.w[h];
+                if constexpr (ODD)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) w[i] = (int)__builtin_amdgcn_alignbyte((uint32_t)(i < 3 ? b.w[h][i < 3 ? i + 1 : i] : b.behind[h]), (uint32_t)b.w[h][i], by);
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
                     intx4 x;
                     if constexpr (OWN) x = *reinterpret_cast<const intx4*>(own_x + (s + d * WAVES) * 128 + h * 64 + g * 16);
                     else x = b.x[j][h];
-                    acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b.w[h], x, acc[j], 0, 0, 0);
+                    acc[j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc[j], 0, 0, 0);
                 }
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     }
@@ -623,9 +643,13 @@ hipError_t launch_lds(K kernel, std::atomic<uint64_t>& raised, unsigned wgs, uns
 }
 template <typename T, int NB, int WAVES, int AHEAD, bool OWN>
 hipError_t rows_launch(const FcI8& P, hipStream_t st) {
-    static std::atomic<uint64_t> raised{0};
-    const unsigned lds = 256 + (unsigned)std::max(OWN ? P.n_tiles * 64 : 0, WAVES * NB * 1024);
-    return launch_lds(fc_i8_rows_kernel<T, NB, WAVES, AHEAD, OWN>, raised, (unsigned)((P.cout + 15) / 16), WAVES * 64, lds, P, st);
+    auto go = [&](auto odd) {
+        constexpr bool ODD = decltype(odd)::value;
+        static std::atomic<uint64_t> raised{0};
+        const unsigned lds = 256 + (unsigned)std::max(OWN ? P.n_tiles * 64 : 0, WAVES * NB * 1024);
+        return launch_lds(fc_i8_rows_kernel<T, NB, WAVES, AHEAD, OWN, ODD>, raised, (unsigned)((P.cout + 15) / 16), WAVES * 64, lds, P, st);
+    };
+    return (reinterpret_cast<uintptr_t>(P.w) | P.K) & 3 ? go(std::true_type()) : go(std::false_type());
 }
 template <typename T, int MT, int NT, int WM, int WN, int STAGES, bool SPLIT = false>
 hipError_t gemm(const FcI8& P, hipStream_t st) {
