@@ -298,7 +298,7 @@ constexpr int kI8FewRows = 64;
 // OWN: there is one row, and every workgroup rounds it itself, into LDS, while its first weights travel, which saves a launch
 // (9216 -> 4096: 9.3 us against 8.6 + 3.1; four rows that way 15.0 against 8.6 + 3.1).  What bounds it: one row 9216 -> 4096 fp32
 // 10.2 us, 3.7 TB/s of weights, of which 2 us are the start of the kernel and the rounding; small layers the way to memory and back, 1152 -> 100
-// 5.4 us; 64 rows (14.0 us, 9216 -> 4096) their 590 KB a CU from L2 and a look-up for every 16 bytes of weights.
+// 5.4 us; 64 rows (9216 -> 4096, where the GEMM takes over, 14.0 us) their 590 KB a CU from L2 and a look-up for every 16 bytes of weights.
 // ODD: rows of weights that begin inside words of 4 bytes: the five words that hold 16 of them (each holds a byte that is asked for), shifted
 // where they are multiplied (loads at such addresses run at half the rate: 9217 -> 4000, one row, 22.7 us, 9216 -> 4000 12.4).
 template <typename T, int NB, int WAVES, int AHEAD, bool OWN, bool ODD>
