@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "dc_fc_quant_plan.h"
 #include "dc_internal.h"
 
 namespace dc {
@@ -289,8 +290,6 @@ __device__ __forceinline__ intx4 weights16(const int8_t* __restrict__ row, int k
     }
     return intx4{(int)(uint32_t)lo, (int)(uint32_t)(lo >> 32), (int)(uint32_t)hi, (int)(uint32_t)(hi >> 32)};
 }
-
-constexpr int kI8FewRows = 64;
 
 // Few rows: a workgroup takes 16 channels x NB * 16 rows.  Its wavefronts deal the 128-byte steps of K among themselves and add
 // their integer sums through LDS.  The weights are what has to come from memory: they go straight from there into fragments
@@ -696,60 +695,29 @@ hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, 
                             : quantize<float, false>((const float*)x, n_rows, K, to, scales, st);
 }
 
-// Workgroups that share a tile of 64 x 64: as many as give every CU one, with eight stages of K each at least.  Putting the sums together
-// costs 2.5 us, so K has to be long: with more than 64 rows (us, alone -> shared) 2048 -> 1000 on 128 rows 10.4 -> 10.7, 4096 -> 1024
-// 14.7 -> 13.4, 9216 -> 4096 30.5 -> 24.9, 25088 -> 512 50.1 -> 28.9; where the other side is the kernel of few rows 4096 -> 4096 on 64
-// rows 14.8 -> 15.5, 9216 -> 4096 23.7 -> 20.7, 25088 -> 512 36.8 -> 27.6, on 17 rows 13.3 -> 15.1, 18.4 -> 18.6, 28.0 -> 25.1.
-static long i8_tiles(int n_rows, int cout) { return ((long)n_rows + 63) / 64 * (((long)cout + 63) / 64); }
-static int i8_splits(int n_rows, int K, int cout) {
-    const int stages = (K + 127) / 128;
-    if (n_rows <= 16 || stages < (n_rows <= kI8FewRows ? 64 : 32)) return 1;
-    return (int)std::max(1l, std::min(256 / i8_tiles(n_rows, cout), (long)stages / 8));
-}
-
-// The workspace: the rows in 8 bits, K padded with zeros to whole steps, their scales, room for weights whose rows are not
-// whole vectors, and the sums and counters of tiles that workgroups share.
-struct I8Space { size_t scales, weights, part, done, end; };
-static I8Space i8_space(int n_rows, int K, int cout) {
-    if (n_rows == 1) return I8Space{0, 0, 0, 0, 0};
-    const size_t row = align_up(K, 128);
-    I8Space s;
-    s.scales = align_up(align_up(n_rows, 16) * row, 256);
-    s.weights = s.scales + align_up((size_t)n_rows * sizeof(float), 256);
-    s.part = s.weights + (n_rows > kI8FewRows ? align_up(cout * row, 256) : 0);
-    const int splits = i8_splits(n_rows, K, cout);
-    s.done = s.part + (splits > 1 ? i8_tiles(n_rows, cout) * splits * (64 * 64 * sizeof(int)) : 0);
-    s.end = s.done + (splits > 1 ? align_up(i8_tiles(n_rows, cout) * sizeof(int32_t), 256) : 0);
-    return s;
-}
-size_t fc_i8_workspace(int n_rows, int K, int cout) { return i8_space(n_rows, K, cout).end; }
+size_t fc_i8_workspace(int n_rows, int K, int cout) { return i8_workspace(n_rows, K, cout); }
 
 template <typename T>
 static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
-    const I8Space space = i8_space(P.n_rows, P.K, P.cout);
-    float* const sx = reinterpret_cast<float*>(ws + space.scales);
-    const int width = (int)align_up(P.K, 128);
+    const I8Plan plan = i8_plan(P.n_rows, P.K, P.cout, P.K % 16 == 0 && reinterpret_cast<uintptr_t>(P.w) % 16 == 0);
+    const int width = (int)plan.width;
     P.x = x; P.n_tiles = width / 64; P.w_stride = P.K;
     if (P.n_rows == 1) return rows_launch<T, 1, 16, 2, true>(P, st);
-    const bool vectors = P.K % 16 == 0 && reinterpret_cast<uintptr_t>(P.w) % 16 == 0;
-    P.splits = i8_splits(P.n_rows, P.K, P.cout);
-    // (the GEMM wants whole vectors: weights of another form are copied for many rows, and few rows have their own kernel)
-    const bool few = P.n_rows <= kI8FewRows && !(P.splits > 1 && vectors);
-    Rows8 to{ws, (size_t)width, width};
-    if (!few && P.splits > 1) {
-        P.part = reinterpret_cast<int*>(ws + space.part);
-        P.done = reinterpret_cast<int32_t*>(ws + space.done);
+    float* const sx = reinterpret_cast<float*>(ws + plan.scales.at);
+    P.splits = plan.splits;
+    Rows8 to{ws + plan.rows.at, plan.width, width};
+    if (plan.splits > 1) {
+        P.part = reinterpret_cast<int*>(ws + plan.part.at);
+        P.done = reinterpret_cast<int32_t*>(ws + plan.done.at);
         to.zero = P.done;
-        to.zeros = (int)i8_tiles(P.n_rows, P.cout);
+        to.zeros = (int)plan.tiles;
     }
-    P.xq = ws; P.x_stride = width; P.sx = sx;
-    hipError_t e = few ? quantize<T, true>(x, P.n_rows, P.K, to, sx, st) : quantize<T, false>(x, P.n_rows, P.K, to, sx, st);
+    P.xq = to.q; P.x_stride = plan.width; P.sx = sx;
+    hipError_t e = plan.few ? quantize<T, true>(x, P.n_rows, P.K, to, sx, st) : quantize<T, false>(x, P.n_rows, P.K, to, sx, st);
     if (e != hipSuccess) return e;
-    if (few) return product_few<T>(P, st);
-    // Rows that begin inside a cache line cost more lines a stage: from 2.5e10 products on padded copies of the weights pay (us, as they are ->
-    // copied: 2064 -> 2048 on 6272 rows 65.0 -> 61.3, 4112 -> 1024 on 12544 123 -> 111; 2064 -> 2048 on 3136 36.8 -> 38.8, 576 -> 256 on 12544 22.5 -> 24.5).
-    if (!vectors || (P.K % 128 && (double)P.n_rows * P.K * P.cout >= 2.5e10)) {
-        int8_t* const w = ws + space.weights;
+    if (plan.few) return product_few<T>(P, st);
+    if (plan.copy) {
+        int8_t* const w = ws + plan.weights.at;
         for (int c = 0; c < P.cout; c += 65535) {
             const int n = std::min(65535, P.cout - c);
             hipLaunchKernelGGL(pad_weights_kernel, dim3((unsigned)((width / 16 + 255) / 256), (unsigned)n), dim3(256), 0, st, P.w + (size_t)c * P.K,
@@ -757,7 +725,7 @@ static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
             e = hipGetLastError();
             if (e != hipSuccess) return e;
         }
-        P.w = w; P.w_stride = width;
+        P.w = w; P.w_stride = plan.width;
     }
     return product_many<T>(P, st);
 }

@@ -1,5 +1,7 @@
 """CPU checks of the 8-bit fully-connected layer's refusals: everything is decided before a kernel is launched."""
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 import torch
@@ -57,3 +59,72 @@ def test_the_binding_refuses_tensors_that_are_not_on_the_gpu():
         binding.dc_fc_quant_layer(x, w, s, None, False)
     with pytest.raises(ValueError):
         binding.dc_quantize_rows(x)
+
+
+# What the launches of one call write, from the kernels' indexing: (area, bytes from its start on).
+_PLAN_CHECK = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "dc_fc_quant_plan.h"
+using namespace dc;
+static int check(int n, int K, int cout, bool vectors, size_t room) {
+    const I8Plan p = i8_plan(n, K, cout, vectors);
+    const size_t width = ((size_t)K + 127) / 128 * 128;
+    auto fail = [&](const char* why) { printf("%s: %d rows, %d -> %d, vectors %d\n", why, n, K, cout, vectors); return 1; };
+    if (p.bytes > room) return fail("more than the query says");
+    if (p.width != width) return fail("row width");
+    if (n == 1) return p.bytes || p.splits != 1 ? fail("one row needs nothing") : 0;
+    if (!p.few && !vectors && !p.copy) return fail("the GEMM takes rows of whole vectors");
+    if (p.few && (n > 64 || p.splits != 1 || p.copy)) return fail("few rows");
+    struct Write { const I8Plan::Area* area; size_t bytes; } w[5] = {
+        // tiles of 16 rows in the one form (what is not a row is read, too), rows in the other
+        {&p.rows, p.few ? ((size_t)n + 15) / 16 * 16 * width : (size_t)n * width},
+        {&p.scales, (size_t)n * 4},
+        {&p.weights, p.copy ? (size_t)cout * width : 0},
+        {&p.part, p.splits > 1 ? ((size_t)n + 63) / 64 * (((size_t)cout + 63) / 64) * p.splits * 64 * 64 * 4 : 0},
+        {&p.done, p.splits > 1 ? ((size_t)n + 63) / 64 * (((size_t)cout + 63) / 64) * 4 : 0}};
+    size_t end = 0;
+    for (const Write& v : w) {
+        if (!v.bytes) continue;
+        if (v.area->at % 256) return fail("alignment");
+        if (v.area->at < end) return fail("areas overlap");
+        end = v.area->at + v.bytes;
+        if (v.bytes > v.area->bytes || end > p.bytes) return fail("written behind the end");
+    }
+    return 0;
+}
+int main(int argc, char** argv) {
+    if (argc == 4) { printf("%zu\n", i8_workspace(atoi(argv[1]), atoi(argv[2]), atoi(argv[3]))); return 0; }
+    const int Ks[] = {1, 15, 16, 17, 100, 128, 1000, 1024, 3968, 3969, 4096, 4097, 4112, 8064, 8065, 8080, 8192, 9216, 9217, 16400, 25088, 50000, 65536, 100001,
+                      131056, 131071, 131072};
+    const int Cs[] = {1, 5, 63, 64, 65, 129, 500, 1000, 2048, 3000, 4096, 5000, 8000, 8192, 8193, 16384, 16448, 40000, 65535, 1 << 20};
+    int bad = 0;
+    for (int i = 0; i < 320; ++i) {
+        const int n = i < 300 ? i + 1 : 300 << (i - 299 < 15 ? i - 299 : 15);
+        for (int K : Ks)
+            for (int c : Cs) {
+                if (((long)n * c) >> 34) continue;
+                const size_t room = i8_workspace(n, K, c);
+                bad += check(n, K, c, false, room);
+                if (K % 16 == 0) bad += check(n, K, c, true, room);
+                if (bad > 10) return 1;
+            }
+    }
+    return bad ? 1 : 0;
+}
+"""
+
+
+def test_every_area_of_a_call_lies_in_its_workspace(tmp_path):
+    """One to 300 rows and many more, lengths and channels up to the limits, weights in whole vectors and not: what the rounding, the
+    copy of the weights and the shared sums write lies apart, and inside what dc_fc_quant_workspace_bytes asks for."""
+    source, exe = tmp_path / "plan.cpp", tmp_path / "plan"
+    source.write_text(_PLAN_CHECK)
+    csrc = os.path.join(os.path.dirname(os.path.abspath(binding.__file__)), "csrc")
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-I", csrc, str(source), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0, out.stdout
+    need = C.c_size_t()
+    for shape in ((1, 100, 8), (40, 100, 8), (64, 50000, 8000), (64, 131056, 3000), (32, 131056, 8000), (17, 8080, 65), (65, 9216, 4096), (300, 4099, 1000)):
+        assert binding.lib().dc_fc_quant_workspace_bytes(*shape, C.byref(need)) == 0
+        assert need.value == int(subprocess.run([str(exe), *map(str, shape)], capture_output=True, text=True, check=True).stdout)

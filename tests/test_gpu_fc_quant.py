@@ -376,3 +376,25 @@ def test_large_products_of_any_row_length(shape):
     got = binding.dc_fc_quant_layer(x, w, s, b, False)
     for r in (0, 1000, n - 64):
         assert torch.equal(got[r:r + 64], binding.dc_fc_quant_layer(x[r:r + 64], w, s, b, False)), r
+
+
+@pytest.mark.parametrize("shape", [(64, 50000, 8000), (33, 131056, 3000)])
+def test_few_rows_of_very_long_weights(shape):
+    """Whole vectors that end inside a cache line, 2.6e10 and 1.3e10 products, at most 64 rows: nothing is written behind the
+    workspace that the query asks for, and the bits are those of 16 rows at a time."""
+    n, k, cout = shape
+    print(f"[fc quant long] {shape}", flush=True)
+    x = _rows(n, k, torch.bfloat16, 1, "relu").to(DEV)
+    w = torch.randint(-127, 128, (cout, k), generator=torch.Generator(device=DEV).manual_seed(2), dtype=torch.int8, device=DEV)
+    s, b = torch.rand(cout, device=DEV) + 0.5, torch.randn(cout, device=DEV)
+    need = binding.C.c_size_t()
+    L = binding.lib()
+    assert L.dc_fc_quant_workspace_bytes(n, k, cout, binding.C.byref(need)) == 0
+    space = torch.full((need.value + (1 << 20),), 77, dtype=torch.uint8, device=DEV)
+    out = torch.empty(n, cout, dtype=torch.bfloat16, device=DEV)
+    assert L.dc_fc_quant_layer(x.data_ptr(), w.data_ptr(), s.data_ptr(), b.data_ptr(), out.data_ptr(), n, k, cout, 0, binding.DC_BF16, space.data_ptr(),
+                               need.value, binding._stream()) == 0
+    torch.cuda.synchronize()
+    assert (space[need.value:] == 77).all()
+    for r in range(0, n, 16):
+        assert torch.equal(out[r:r + 16], binding.dc_fc_quant_layer(x[r:r + 16], w, s, b, False).view(-1, cout)), r
