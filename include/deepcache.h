@@ -264,6 +264,7 @@ int32_t dc_overlap_pipeline(void* overlap, int32_t frames_in_flight /* 1 or 2 */
  * whose launches take the host longer than the GPU takes per frame are recorded as HIP graphs and replayed; whether
  * that is so is measured.  dc_overlap_replay decides instead: 0 never, 1 always, -1 measured (the default).  Frames
  * that cannot be replayed (planned on the host, with a profile, with lists or origins read back) are launched as ever.
+ * A call that replays may wait until the GPU is less than 24 frames behind.
  * Results do not depend on it but for the grouping of split sums: launch shapes follow the lengths of the lists as
  * the last frames had them, a recorded frame's those at its recording.  Errors: DC_ERR_NULL_PTR, DC_ERR_INVALID_ARG.
  */

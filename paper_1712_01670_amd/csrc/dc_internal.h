@@ -331,6 +331,7 @@ struct Profile {
 // the same frame (one event) and stage s of frame f - 1 (same stream, no event).  A layer's cache is the previous
 // frame's output of the same layer, hence of the same stage, so the frames in flight need no waits per layer.
 constexpr int kMaxStages = 4;              // streams: the process has four hardware queues
+constexpr int kMarkFrames = 8;            // replayed frames between two marks that the host waits for
 constexpr int kFramesInFlight = 4;         // plan areas and frame records that take turns
 struct FrameGraphs;
 struct StackPlan;                          // what dc_run_stack derives from a stack's description (dc_stack.hip)
@@ -361,6 +362,7 @@ struct Overlap {
     int parity = 0;
     bool pipeline = false;
     FrameRecord ring[kFramesInFlight];
+    hipEvent_t mark[2] = {nullptr, nullptr};          // end of a replayed frame, kMarkFrames before the other
     uint64_t frame_no = 0;
     hipStream_t head = nullptr;                       // stream of the last frame's matching and planning on the GPU
     std::vector<StackPlan*> plans;                    // most recently used first

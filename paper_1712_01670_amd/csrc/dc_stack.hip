@@ -772,6 +772,7 @@ struct StackCall {
     int emit_stage(int s, hipStream_t st);
     dc::FrameGraphs* find_graphs();
     int record_graphs(dc::FrameGraphs& g);
+    bool replays() const;
     int run();
     hipError_t wait(hipStream_t st, hipEvent_t e) const { return hipStreamWaitEvent(st, e, 0); }     // free when e is complete
     bool prefetched() const {
@@ -901,6 +902,15 @@ int StackCall::begin() {
         const hipEvent_t end = prev.done[prev.n_stages - 1];
         for (int s = 0; s < k; ++s) DC_TRY_HIP(wait(stage_st[s], end));
         DC_TRY_HIP(wait(ov->aux, end));
+    }
+    // A replayed frame costs the host next to nothing, so that nothing else would keep it from running ahead of the GPU without
+    // end, and a recording would be kept and replayed long after the lists have changed.  So once in kMarkFrames the host
+    // waits for what it replayed 2 kMarkFrames before, which takes no time; the stages have up to four frames at work (waiting at
+    // every frame for the fourth before: Darknet-19 0.126 -> 0.133 ms a frame).
+    if (ov->frame_no % kMarkFrames == 0 && replays()) {
+        const hipEvent_t mark = ov->mark[ov->frame_no / kMarkFrames % 2];
+        const Blocked b(*this);
+        if (mark) DC_TRY_HIP(spin_wait(mark));
     }
     return DC_OK;
 }
@@ -1368,13 +1378,17 @@ constexpr int kGraphUses = 2;               // frames of a key that are launched
 constexpr int kGraphOffShape = 8;           // consecutive frames with other list lengths before a graph is recorded anew:
 constexpr int kGraphOffUnits = 16;          // a layer's differs by more than a quarter and this many units (the launch of a few is as good as any)
 
+// Whether recorded frames are replayed, of this call's kind: nothing may wait for the host in between.
+bool StackCall::replays() const {
+    const bool wanted = ov && (ov->replay_mode < 0 ? P.replay.on && !P.replay.refresh() : ov->replay_mode == 1 && opt && P.device_plan);
+    if (!pipe || !wanted || (cached && !devplan) || prof || regions_out || P.no_graphs) return false;
+    return std::none_of(std::begin(P.tight), std::end(P.tight), [](bool tight) { return tight; });      // (a wait in the middle of a stage)
+}
+
 // The entry for this frame's key, or nullptr if the frame cannot be replayed from a graph: everything its kernels take
 // as arguments has to be part of the key, and nothing may wait for the host or go through a copy in between.
 dc::FrameGraphs* StackCall::find_graphs() {
-    const bool wanted = ov && (ov->replay_mode < 0 ? P.replay.on && !P.replay.refresh() : ov->replay_mode == 1 && opt && P.device_plan);
-    if (!pipe || !wanted || (cached && !devplan) || prof || regions_out || P.no_graphs) return nullptr;
-    for (bool tight : P.tight)      // (a wait in the middle of a stage)
-        if (tight) return nullptr;
+    if (!replays()) return nullptr;
     if (cached && (!host_alias || (P.torus && opt->origins_out))) return nullptr;
     const size_t n = n_layers;
     std::vector<uint64_t> key;
@@ -1582,6 +1596,11 @@ int StackCall::run() {
         rec->timed = timed;
         rec->tail = false;
         rec->valid = true;
+        if (replay && ov->frame_no % kMarkFrames == 0) {
+            hipEvent_t& mark = ov->mark[ov->frame_no / kMarkFrames % 2];
+            if (!mark) DC_TRY_HIP(hipEventCreateWithFlags(&mark, hipEventDisableTiming));
+            DC_TRY_HIP(hipEventRecord(mark, stage_st[k - 1]));
+        }
         ++ov->frame_no;
         ++ov->counters.frames;
         ov->counters.replayed += replay ? 1 : 0;
@@ -1631,6 +1650,8 @@ int32_t dc_overlap_destroy(void* overlap) {
         }
     for (FrameRecord& r : o->ring)
         if (r.after) (void)hipEventDestroy(r.after);
+    for (hipEvent_t e : o->mark)
+        if (e) (void)hipEventDestroy(e);
     if (o->match_done) (void)hipEventDestroy(o->match_done);
     if (o->plan_done) (void)hipEventDestroy(o->plan_done);
     if (o->record) (void)hipStreamDestroy(o->record);

@@ -1125,6 +1125,44 @@ def test_a_recording_is_dropped_for_one_layer_alone():
         assert torch.equal(x, y)
 
 
+def test_replayed_frames_do_not_run_far_ahead_of_the_gpu():
+    """A caller with long work of its own behind every frame, which a replayed frame's launches would leave far behind: the
+    host is at most 24 frames ahead, so that a recording whose lists have changed is made anew within a few dozen frames."""
+    layers = synth.vgg16()[:10]
+    ws, bs = synth.he_weights(layers, 3, bias_scale=0.05, input_shape=(96, 96, 3))
+    rng = np.random.default_rng(10)
+    still = rng.integers(0, 256, (1, 96, 96, 3), np.uint8)
+    part = [still.copy() for _ in range(4)]
+    for k, p in enumerate(part):
+        p[0, 8 * k:8 * k + 8, 30:40] = rng.integers(0, 256, (8, 10, 3), np.uint8)
+    frames = [torch.from_numpy(v).to(DEV) for v in part + [rng.integers(0, 256, (1, 96, 96, 3), np.uint8) for _ in range(4)]]
+    work = torch.ones(4096, 4096, device=DEV)
+    torch.cuda.synchronize()
+    order = [j % 4 for j in range(60)] + [4 + j % 4 for j in range(90)] + [None]
+    ends, late = [], []
+
+    def before(j, runner):
+        if j >= 26 and runner.overlap_counters().replayed > replays[-1]:     # the last step was replayed: the one 26 before this is over
+            late.append(not ends[j - 26].query())
+        replays.append(runner.overlap_counters().replayed)
+        ends.append(torch.cuda.Event())
+        ends[-1].record()
+        torch.mm(work, work)                                                 # behind the last frame, before this one's last layers
+
+    binding.dc_conv_tuning(0, 4, 1, 0)
+    try:
+        replays = [0]
+        kept, c, _ = _replay_run(layers, ws, bs, frames, 16, False, 1, order, before=before)
+        plain, _, _ = _replay_run(layers, ws, bs, frames, 16, False, 0, order)
+    finally:
+        binding.dc_conv_tuning()
+    print("[far ahead]", [(n, getattr(c, n)) for n, _ in c._fields_], sum(late), len(late), flush=True)
+    assert len(late) > 50 and not any(late)
+    assert c.failed == 0 and c.dropped >= 1 and c.recorded > c.dropped
+    for x, y in zip(kept[0], plain[0]):
+        assert torch.equal(x, y)
+
+
 def test_frames_of_more_blocks_than_the_gpu_plans_run_as_host_planned():
     """A frame of more than 64 blocks per row is planned on the host whatever device_plan says: same tensors bit for bit as
     without the option, and the same pipeline: no stage of layers on the stream of the matching, which the host waits for."""
