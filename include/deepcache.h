@@ -583,7 +583,8 @@ int32_t dc_stack_workspace_bytes(const dc_layer* layers, int32_t n_layers, int32
  *   packed_weights  optional (NULL) host array [n_layers] of dev pointers: packed copies of the
  *                   weights (NULL entries for layers without one); a DC_FC layer's entry is a block of
  *                   dc_pack_fc_weights and makes it a layer in 8-bit integers (its rows of up to 131072
- *                   values are rounded into the scratch areas of ws_dev: DC_ERR_WORKSPACE if they do not fit)
+ *                   values are rounded into the scratch areas of ws_dev, for more than one stream DC_ERR_WORKSPACE
+ *                   without one of dc_stack_workspace_bytes)
  *   frames_cur      dev u8 [n_streams][H][W][C]
  *   frames_prev     dev u8, previous frames (cache keys); ignored when force_full
  *   tensors_cur     host array [n_layers+1] of dev pointers, every tensor of this frame

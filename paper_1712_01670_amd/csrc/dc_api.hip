@@ -697,7 +697,7 @@ int32_t dc_fc_quant_layer(const void* in, const int8_t* weights, const float* we
     if (need && !ws_dev) return DC_ERR_NULL_PTR;
     if (ws_dev_bytes < need) return DC_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(ws_dev) % 256 || in == out) return DC_ERR_INVALID_ARG;
-    DC_TRY_HIP(launch_fc_i8(in, weights, weight_scales, bias, out, n_rows, (int)K, cout, relu, dtype, ws_dev, as_stream(stream)));
+    DC_TRY_HIP(launch_fc_i8(in, weights, weight_scales, bias, out, n_rows, (int)K, cout, relu, dtype, ws_dev, ws_dev_bytes, as_stream(stream)));
     return DC_OK;
 }
 

@@ -697,9 +697,12 @@ hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, 
 
 size_t fc_i8_workspace(int n_rows, int K, int cout) { return i8_workspace(n_rows, K, cout); }
 
+static bool whole_vectors(const int8_t* w, int K) { return K % 16 == 0 && reinterpret_cast<uintptr_t>(w) % 16 == 0; }
+int fc_i8_rows(int n_rows, int K, int cout, const int8_t* w, size_t ws_bytes) { return i8_rows(n_rows, K, cout, whole_vectors(w, K), ws_bytes); }
+
 template <typename T>
-static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
-    const I8Plan plan = i8_plan(P.n_rows, P.K, P.cout, P.K % 16 == 0 && reinterpret_cast<uintptr_t>(P.w) % 16 == 0);
+static hipError_t run_fc_i8(const T* x, FcI8 P, int8_t* ws, size_t ws_bytes, hipStream_t st) {
+    const I8Plan plan = i8_plan(P.n_rows, P.K, P.cout, whole_vectors(P.w, P.K), ws_bytes);
     const int width = (int)plan.width;
     P.x = x; P.n_tiles = width / 64; P.w_stride = P.K;
     if (P.n_rows == 1) return rows_launch<T, 1, 16, 2, true>(P, st);
@@ -731,11 +734,20 @@ static hipError_t run_fc_i8(const T* x, FcI8& P, int8_t* ws, hipStream_t st) {
 }
 
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
-                        int dtype, void* ws, hipStream_t st) {
-    FcI8 P;
-    P.w = w; P.sw = sw; P.bias = bias; P.out = out;
-    P.n_rows = n_rows; P.K = K; P.cout = cout; P.relu = relu;
-    return dtype == DC_BF16 ? run_fc_i8((const __hip_bfloat16*)x, P, static_cast<int8_t*>(ws), st) : run_fc_i8((const float*)x, P, static_cast<int8_t*>(ws), st);
+                        int dtype, void* ws, size_t ws_bytes, hipStream_t st) {
+    const int at_once = fc_i8_rows(n_rows, K, cout, w, ws_bytes);
+    if (at_once < 1) return hipErrorInvalidValue;
+    for (int r = 0; r < n_rows; r += at_once) {
+        FcI8 P;
+        P.w = w; P.sw = sw; P.bias = bias; P.K = K; P.cout = cout; P.relu = relu;
+        P.n_rows = std::min(at_once, n_rows - r);
+        P.out = static_cast<unsigned char*>(out) + (size_t)r * cout * dtype_size(dtype);
+        const void* const rows = static_cast<const unsigned char*>(x) + (size_t)r * K * dtype_size(dtype);
+        const hipError_t e = dtype == DC_BF16 ? run_fc_i8((const __hip_bfloat16*)rows, P, static_cast<int8_t*>(ws), ws_bytes, st)
+                                              : run_fc_i8((const float*)rows, P, static_cast<int8_t*>(ws), ws_bytes, st);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace dc

@@ -34,8 +34,9 @@ inline int i8_splits(int n_rows, int K, long tiles) {
 }
 
 // vectors: rows of weights are whole 16-byte vectors (K and their address are multiples of 16), as the GEMM wants them: weights of
-// another form are copied for many rows, and few rows have their own kernel.
-inline I8Plan i8_plan(int n_rows, int K, int cout, bool vectors) {
+// another form are copied for many rows, and few rows have their own kernel.  room: bytes of the workspace; a copy that only saves
+// time is made if they suffice for it.
+inline I8Plan i8_plan(int n_rows, int K, int cout, bool vectors, size_t room = SIZE_MAX) {
     auto up = [](size_t v, size_t a) { return (v + a - 1) / a * a; };
     I8Plan p;
     p.width = up(K, 128);
@@ -44,21 +45,35 @@ inline I8Plan i8_plan(int n_rows, int K, int cout, bool vectors) {
     const int splits = i8_splits(n_rows, K, p.tiles);
     p.few = n_rows <= kI8FewRows && !(splits > 1 && vectors);
     if (!p.few) p.splits = splits;
+    auto lay_out = [&](bool copy) {
+        p.copy = copy;
+        p.bytes = 0;
+        auto take = [&](size_t bytes) {
+            const I8Plan::Area a{p.bytes, bytes};
+            p.bytes += up(bytes, 256);
+            return a;
+        };
+        p.rows = take(up(n_rows, 16) * p.width);
+        p.scales = take((size_t)n_rows * sizeof(float));
+        p.weights = take(copy ? cout * p.width : 0);
+        p.part = take(p.splits > 1 ? p.tiles * p.splits * (kI8TileSums * sizeof(int32_t)) : 0);
+        p.done = take(p.splits > 1 ? p.tiles * sizeof(int32_t) : 0);
+    };
     // Rows that begin inside a cache line cost more lines a stage: from 2.5e10 products on padded copies of the weights pay (us, as they are ->
     // copied: 2064 -> 2048 on 6272 rows 65.0 -> 61.3, 4112 -> 1024 on 12544 123 -> 111; 2064 -> 2048 on 3136 36.8 -> 38.8, 576 -> 256 on 12544 22.5 -> 24.5).
     // Up to 64 rows read every weight once, and a copy would read and write it besides.
-    p.copy = n_rows > kI8FewRows && (!vectors || (K % 128 && (double)n_rows * K * cout >= 2.5e10));
-    auto take = [&](size_t bytes) {
-        const I8Plan::Area a{p.bytes, bytes};
-        p.bytes += up(bytes, 256);
-        return a;
-    };
-    p.rows = take(up(n_rows, 16) * p.width);
-    p.scales = take((size_t)n_rows * sizeof(float));
-    p.weights = take(p.copy ? cout * p.width : 0);
-    p.part = take(p.splits > 1 ? p.tiles * p.splits * (kI8TileSums * sizeof(int32_t)) : 0);
-    p.done = take(p.splits > 1 ? p.tiles * sizeof(int32_t) : 0);
+    const bool many = n_rows > kI8FewRows;
+    lay_out(many && (!vectors || (K % 128 && (double)n_rows * K * cout >= 2.5e10)));
+    if (p.copy && vectors && p.bytes > room) lay_out(false);
     return p;
+}
+
+// Rows that a workspace of `room` bytes serves at once: all of them, or 64 at a time, which copy no weights (0: not even those).  A row's
+// result does not depend on the others, nor on which kernel computes it.
+inline int i8_rows(int n_rows, int K, int cout, bool vectors, size_t room) {
+    for (int n : {n_rows, std::min(n_rows, kI8FewRows)})
+        if (i8_plan(n, K, cout, vectors, room).bytes <= room) return n;
+    return 0;
 }
 
 // What a call needs whatever its weights' address.

@@ -197,8 +197,10 @@ constexpr size_t kI8MaxK = 131072;       // 127 * 127 * K < 2^31
 // q [n_rows][K], scales [n_rows]
 hipError_t launch_quantize_rows(const void* x, int dtype, size_t n_rows, int K, int8_t* q, float* scales, hipStream_t st);
 size_t fc_i8_workspace(int n_rows, int K, int cout);
+// In a smaller workspace than fc_i8_workspace the rows are taken a part at a time: so many at once, or 0 if it is too small for any.
+int fc_i8_rows(int n_rows, int K, int cout, const int8_t* w, size_t ws_bytes);
 hipError_t launch_fc_i8(const void* x, const int8_t* w, const float* sw, const float* bias, void* out, int n_rows, int K, int cout, int relu,
-                        int dtype, void* ws, hipStream_t st);
+                        int dtype, void* ws, size_t ws_bytes, hipStream_t st);
 inline size_t packed_fc_scales(size_t K, int cout) { return align_up(K * cout, 16); }      // where they start
 // ---- mixture-of-experts layer (dc_moe.hip) ----
 constexpr int kMoeMaxExperts = 256, kMoeMaxTopK = 16, kMoeMaxTokens = 512;

@@ -874,8 +874,8 @@ int StackCall::begin() {
         const size_t K = (size_t)P.hs[l.in0] * P.ws[l.in0] * P.cs[l.in0];
         if (K > kI8MaxK) return DC_ERR_UNSUPPORTED;
         if (reinterpret_cast<uintptr_t>(packed[i]) % 16) return DC_ERR_INVALID_ARG;
-        const size_t need = fc_i8_workspace(n_streams, (int)K, l.cout);
-        if (need && (!scratch || need > kConvScratchBytes || reinterpret_cast<uintptr_t>(scratch) % 16)) return DC_ERR_WORKSPACE;
+        const size_t room = scratch && reinterpret_cast<uintptr_t>(scratch) % 16 == 0 ? kConvScratchBytes : 0;
+        if (!fc_i8_rows(n_streams, (int)K, l.cout, static_cast<const int8_t*>(packed[i]), room)) return DC_ERR_WORKSPACE;
     }
     devplan = cached && P.device_plan &&
               align_up(P.dl.table_bytes, 256) + P.dl.frame_bytes <= area_bytes && ws_host_bytes >= kDevHostRegion + 256;
@@ -1324,7 +1324,8 @@ int StackCall::emit_layer(int i, hipStream_t st, ConvAdd* add, ConvBatch* batch)
                 const size_t K = (size_t)hs[a] * ws[a] * cs[a];
                 const unsigned char* const block = static_cast<const unsigned char*>(packed[i]);
                 DC_TRY_HIP(launch_fc_i8(eff[a], reinterpret_cast<const int8_t*>(block), reinterpret_cast<const float*>(block + packed_fc_scales(K, l.cout)),
-                                        bias ? bias[i] : nullptr, eff[t], n_streams, (int)K, l.cout, l.relu != 0, dtype, stage_scratch(i), st));
+                                        bias ? bias[i] : nullptr, eff[t], n_streams, (int)K, l.cout, l.relu != 0, dtype, stage_scratch(i),
+                                        scratch ? kConvScratchBytes : 0, st));
                 return DC_OK;
             }
             DC_TRY_HIP(launch_fc(eff[a], weights[i], bias ? bias[i] : nullptr, eff[t], n_streams, (size_t)hs[a] * ws[a] * cs[a], l.cout, l.relu, dtype, st));

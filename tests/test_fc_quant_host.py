@@ -68,7 +68,7 @@ _PLAN_CHECK = r"""
 #include "dc_fc_quant_plan.h"
 using namespace dc;
 static int check(int n, int K, int cout, bool vectors, size_t room) {
-    const I8Plan p = i8_plan(n, K, cout, vectors);
+    const I8Plan p = i8_plan(n, K, cout, vectors, room);
     const size_t width = ((size_t)K + 127) / 128 * 128;
     auto fail = [&](const char* why) { printf("%s: %d rows, %d -> %d, vectors %d\n", why, n, K, cout, vectors); return 1; };
     if (p.bytes > room) return fail("more than the query says");
@@ -95,6 +95,7 @@ static int check(int n, int K, int cout, bool vectors, size_t room) {
 }
 int main(int argc, char** argv) {
     if (argc == 4) { printf("%zu\n", i8_workspace(atoi(argv[1]), atoi(argv[2]), atoi(argv[3]))); return 0; }
+    if (i8_rows(5, 131072, 8, true, 100000) || i8_rows(1, 131072, 8, true, 0) != 1) return 2;
     const int Ks[] = {1, 15, 16, 17, 100, 128, 1000, 1024, 3968, 3969, 4096, 4097, 4112, 8064, 8065, 8080, 8192, 9216, 9217, 16400, 25088, 50000, 65536, 100001,
                       131056, 131071, 131072};
     const int Cs[] = {1, 5, 63, 64, 65, 129, 500, 1000, 2048, 3000, 4096, 5000, 8000, 8192, 8193, 16384, 16448, 40000, 65535, 1 << 20};
@@ -107,6 +108,12 @@ int main(int argc, char** argv) {
                 const size_t room = i8_workspace(n, K, c);
                 bad += check(n, K, c, false, room);
                 if (K % 16 == 0) bad += check(n, K, c, true, room);
+                // the 32 MiB that a layer of a stack has, whatever its size: all rows at once, or parts
+                for (int vectors = 0; vectors <= (K % 16 == 0); ++vectors) {
+                    const int part = i8_rows(n, K, c, vectors, 32 << 20);
+                    if (part != n && part != 64) { printf("%d rows at once: %d, %d -> %d\n", part, n, K, c); ++bad; }
+                    else bad += check(part, K, c, vectors, 32 << 20) + (n % part ? check(n % part, K, c, vectors, 32 << 20) : 0);
+                }
                 if (bad > 10) return 1;
             }
     }

@@ -398,3 +398,23 @@ def test_few_rows_of_very_long_weights(shape):
     assert (space[need.value:] == 77).all()
     for r in range(0, n, 16):
         assert torch.equal(out[r:r + 16], binding.dc_fc_quant_layer(x[r:r + 16], w, s, b, False).view(-1, cout)), r
+
+
+@pytest.mark.parametrize("dtype", [binding.DC_F32, binding.DC_BF16])
+@pytest.mark.parametrize("size,channels,n", [(32, 16, 70), (31, 17, 130)])
+def test_a_stack_of_many_streams(size, channels, n, dtype):
+    """More than 64 streams, and a head whose weights are more than a stage's scratch memory: rows of whole vectors, which need no copy of
+    them, and rows of an odd length, which are taken 64 streams at a time.  Bits of the single call."""
+    print(f"[stack of many streams] {size} {channels} {n} {dtype}", flush=True)
+    layers = synth._chain([("c", channels, 3, 1, 1)], 3)
+    layers += [synth._fc(channels, 2200, True, 1), synth._fc(2200, 30, False, 2)]
+    ws, bs = synth.he_weights(layers, 5, bias_scale=0.05, input_shape=(size, size, 3))
+    assert ws[1].size > 33 << 20
+    runner = binding.StackRunner(layers, ws, bs, n, size, size, 3, dtype=dtype, fc_quant=True)
+    frame = torch.randint(0, 256, (n, size, size, 3), dtype=torch.uint8, generator=torch.Generator().manual_seed(3)).to(DEV)
+    for _ in range(2):
+        got = runner.step(frame)
+        torch.cuda.synchronize()
+        for i in (1, 2):
+            q, s = binding.dc_quantize_rows(runner.w[i].reshape(runner.w[i].shape[0], -1))
+            assert torch.equal(got[i + 1].view(n, 1, 1, -1), binding.dc_fc_quant_layer(got[i], q, s, runner.b[i], i == 1)), i
