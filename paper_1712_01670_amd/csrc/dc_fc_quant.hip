@@ -260,9 +260,24 @@ __device__ __forceinline__ float to_out<float>(float v) { return v; }
 template <>
 __device__ __forceinline__ __hip_bfloat16 to_out<__hip_bfloat16>(float v) { return __float2bfloat16(v); }
 
-// A sum's way out, the same operations in every kernel.
-__device__ __forceinline__ float finish(int sum, float sw, float sx, float bias, int relu) {
-    const float v = fmaf((float)sum * sw, sx, bias);
+// A sum's way out, the same operations in every kernel.  The sum has 31 bits: its product with a very large scale of weights would leave
+// fp32 where the result, with a small scale of the row, does not.  Such a scale is taken 2^-64 times and the row's 2^64 times
+// (finite: a sum of zero stays one).  (In the other direction nothing is lost: a whole number times the smallest number is exact.)
+struct WeightScale {
+    float s;
+    bool large;
+    __device__ __forceinline__ explicit WeightScale(float sw) : s(sw), large(fabsf(sw) > 0x1p90f) {
+        if (large) s = sw * 0x1p-64f;
+    }
+};
+struct OutScale {              // of a row
+    float s, behind_large;
+    __device__ __forceinline__ explicit OutScale(float sx) : s(sx), behind_large(sx * 0x1p64f) {
+        if (behind_large > 0x1.fffffep127f) behind_large = 0x1.fffffep127f;
+    }
+};
+__device__ __forceinline__ float finish(int sum, const WeightScale& sw, const OutScale& sx, float bias, int relu) {
+    const float v = fmaf((float)sum * sw.s, sw.large ? sx.behind_large : sx.s, bias);
     return relu && v < 0.f ? 0.f : v;
 }
 
@@ -435,12 +450,12 @@ __global__ __launch_bounds__(WAVES * 64) void fc_i8_rows_kernel(FcI8 P) {
         intx4 sum = red[i];
 #pragma unroll
         for (int v = 1; v < WAVES; ++v) sum += red[v * NB * 64 + i];
-        const float sx = OWN ? own_scale : P.sx[row];
+        const OutScale sx(OWN ? own_scale : P.sx[row]);
         T* const out = static_cast<T*>(P.out) + (size_t)row * P.cout;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (o + e >= P.cout) break;
-            out[o + e] = to_out<T>(finish(sum[e], P.sw[o + e], sx, P.bias ? P.bias[o + e] : 0.f, P.relu));
+            out[o + e] = to_out<T>(finish(sum[e], WeightScale(P.sw[o + e]), sx, P.bias ? P.bias[o + e] : 0.f, P.relu));
         }
     }
 }
@@ -598,18 +613,17 @@ __global__ __launch_bounds__(WM * WN * 64) void fc_i8_gemm_kernel(FcI8 P) {
     for (int j = 0; j < UN; ++j) {
         const int o = o0 + (wn * UN + j) * 16 + g * 4;
         if (o >= P.cout) continue;
-        floatx4 sw, bias{0.f, 0.f, 0.f, 0.f};
+        const auto channel = [&](int e) { return min(o + e, P.cout - 1); };
+        const WeightScale sw[4] = {WeightScale(P.sw[channel(0)]), WeightScale(P.sw[channel(1)]), WeightScale(P.sw[channel(2)]), WeightScale(P.sw[channel(3)])};
+        floatx4 bias{0.f, 0.f, 0.f, 0.f};
+        if (P.bias)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int c = min(o + e, P.cout - 1);
-            sw[e] = P.sw[c];
-            if (P.bias) bias[e] = P.bias[c];
-        }
+            for (int e = 0; e < 4; ++e) bias[e] = P.bias[channel(e)];
 #pragma unroll
         for (int i = 0; i < UM; ++i) {
             const int row = m0 + (wm * UM + i) * 16 + l16;
             if (row >= P.n_rows) continue;
-            const float sx = P.sx[row];
+            const OutScale sx(P.sx[row]);
             T v[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = to_out<T>(finish(acc[i][j][e], sw[e], sx, bias[e], P.relu));

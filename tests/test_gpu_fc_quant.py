@@ -418,3 +418,28 @@ def test_a_stack_of_many_streams(size, channels, n, dtype):
         for i in (1, 2):
             q, s = binding.dc_quantize_rows(runner.w[i].reshape(runner.w[i].shape[0], -1))
             assert torch.equal(got[i + 1].view(n, 1, 1, -1), binding.dc_fc_quant_layer(got[i], q, s, runner.b[i], i == 1)), i
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("n", [1, 5, 64, 70, 300])
+def test_scales_at_opposite_ends_of_the_range(n, dtype):
+    """Large weights for small rows and the other way round: the product of the sum and one scale leaves fp32, the result does not."""
+    k, cout = 5000, 130
+    x = _rows(n, k, dtype, n, "relu")
+    w, s, b = _weights(cout, k, 2)
+    w[5] = 0
+    for row, weight in ((1e-30, 1e41), (1e-25, 1e38), (2.0 ** -95, 2.0 ** 135), (1e30, 1e-34), (1e20, 1e-40), (2.0 ** 110, 2.0 ** -100)):
+        xs, ss = (x.double() * row).to(dtype), (s.double() * weight).float()
+        ss[::7] = s[::7]                             # ordinary channels beside them,
+        ss[3] = 0                                    # and one without weights
+        got = binding.dc_fc_quant_layer(xs.to(DEV), w.to(DEV), ss.to(DEV), b.to(DEV), False)
+        terms = np.abs(_expected(xs, w, ss, None, False)) + b.double().abs().numpy()
+        assert np.isfinite(terms).all() and terms.max() < 1e38
+        _check(got, _expected(xs, w, ss, b, False), dtype, terms)
+    # both large: the outputs are infinite where there is anything, and a sum of zero gives the bias
+    xs, ss = (x.double() * 1e30).to(dtype), (s.double() * 1e41).float()
+    got = binding.dc_fc_quant_layer(xs.to(DEV), w.to(DEV), ss.to(DEV), b.to(DEV), False).cpu().view(n, cout)
+    q, _ = _quantized(xs)
+    sums = q @ w.double().numpy().T
+    assert torch.equal(got[:, 5], b[5].to(dtype).expand(n))
+    assert (got.double().numpy()[sums != 0] == np.sign(sums[sums != 0]) * np.inf).all()
