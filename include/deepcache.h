@@ -534,7 +534,8 @@ int32_t dc_pack_fc_weights(const void* weights, size_t K, int32_t cout, int32_t 
  *   h_e = relu(up_e x + up_bias_e)                                         act = DC_MOE_RELU
  *   h_e = silu(u) * v with u, v the halves of up_e x + up_bias_e           act = DC_MOE_GATED, silu(u) = u / (1 + exp(-u))
  *   out = sum over the chosen e of gate_e (down_e h_e + down_bias_e)
- * All sums are held in fp32 (h_e too: in bf16 as two numbers each) and the output is rounded once.  An expert whose logit is
+ * All sums are held in fp32 (h_e too: in bf16 as two numbers each; with DC_I8 they are sums of whole numbers times x or h_e, the
+ * scale behind them) and the output is rounded once.  An infinite weight of `down` in bf16 makes its outputs NaN.  An expert whose logit is
  * -inf (a router_bias of -inf switches an expert off) is never chosen; a token left with fewer than top_k experts has the
  * expert -1 and the gate 0 in the last places, one left with none an output of zeros.  A NaN among a token's logits makes its
  * gates and its output NaN and leaves the other tokens alone.

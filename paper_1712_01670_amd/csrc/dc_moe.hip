@@ -689,6 +689,8 @@ __global__ __launch_bounds__(kMoeWaves * 64) void moe_expert_kernel(Moe P) {
                     else v = u > 0.f || u != u ? u : 0.f;
                     if (c0 + q >= P.hidden) v = 0.f;           // behind the last channel the second layer multiplies zeros
                     store(&high[q], v);
+                    if constexpr (PLANES == 2)
+                        if (fabsf(v) < INFINITY && (high[q] & 0x7fff) == 0x7f80) --high[q];      // (a number that rounds to infinity: the largest below)
                     const float h = to_float(high[q]);
                     store(&rest[q], fabsf(h) < INFINITY || h != h ? v - h : 0.f);
                 }

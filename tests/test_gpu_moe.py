@@ -309,3 +309,20 @@ def test_scales_beside_weights_that_have_none_are_refused():
     c["up_scale"] = torch.ones(4, 32)
     with pytest.raises(ValueError):
         _call(c)
+
+
+@pytest.mark.parametrize("n", [3, 20, 40])
+def test_hidden_values_next_to_the_largest_number_stay_finite(n):
+    """Hidden values that fp32 holds and bf16 would round to infinity, of either sign, behind both kinds of first layers.  (Not with 8-bit
+    weights: their sums are of whole numbers, 127 times such a value is no number of fp32.)"""
+    for gated in (False, True):
+        c = _case(n, 3, 2, 32, 40, 24, "bf16", "bf16", gated=gated, bias=True)
+        c["x"][:] = 0
+        c["up_bias"][:] = 3.4e38
+        if gated:
+            c["up_bias"][:, :40], c["up_bias"][:, 40:] = 100.0, 3.4e36
+            c["up_bias"][:, 41::2] *= -1
+        c["down"] *= 1e-32
+        got = _call(c)
+        assert torch.isfinite(got[0].float()).all()
+        _check(c, got)
