@@ -443,3 +443,47 @@ def test_scales_at_opposite_ends_of_the_range(n, dtype):
     sums = q @ w.double().numpy().T
     assert torch.equal(got[:, 5], b[5].to(dtype).expand(n))
     assert (got.double().numpy()[sums != 0] == np.sign(sums[sums != 0]) * np.inf).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(8300, 200, 50), (8200, 208, 64), (3100, 528, 1000), (3137, 515, 900), (12400, 272, 4090), (12300, 259, 4100),
+                                   (4100, 272, 1300), (70, 33, 70000), ((1 << 20) + 30, 17, 5)])
+def test_products_of_many_tiles(shape, dtype):
+    """The GEMM's other tiles, with ragged rows and channels and rows of weights in whole vectors and not: 128 x 64 (up to 64
+    channels), 128 x 128 in three stages (as many tiles as CUs) and in two, 256 x 256 (many); more channels than a launch of the
+    copy has, and more rows than a launch of the rounding.  Rows from every part, the last tile's among them."""
+    n, k, cout = shape
+    print(f"[fc quant tiles] {shape} {dtype}", flush=True)
+    x = _rows(n, k, dtype, n, "relu")
+    w, s, b = _weights(cout, k, 3)
+    rows = torch.unique(torch.cat([torch.arange(0, n, n // 40), torch.arange(n - 20, n)]))
+    for bias, relu in ((b, True), (None, False)):
+        got = binding.dc_fc_quant_layer(x.to(DEV), w.to(DEV), s.to(DEV), None if bias is None else bias.to(DEV), relu).cpu()[rows]
+        assert got.shape == (len(rows), 1, 1, cout)
+        plain = _expected(x[rows], w, s, None, False)
+        want = _expected(x[rows], w, s, bias, relu)
+        _check(got, want, dtype, np.abs(plain) + (0 if bias is None else np.abs(bias.double().numpy())) + np.abs(want))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("k", [300, 1000, 2001, 4090, 8191, 20000])
+def test_many_quantized_rows_are_exact(k, dtype):
+    """Every number of lanes that share a row of many, and rows that are read in two passes of a workgroup."""
+    print(f"[quantize many] {k} {dtype}", flush=True)
+    x = _rows(2051, k, dtype, k)
+    q, s = binding.dc_quantize_rows(x.to(DEV))
+    want_q, want_s = _quantized(x)
+    assert (s.cpu().numpy() == want_s).all() and (q.cpu().numpy() == want_q).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(3, 131072, 5), (16, 70001, 9), (40, 100001, 7), (60, 70001, 37), (70, 70001, 33), (70, 131072, 3)])
+def test_rows_that_are_read_twice(shape, dtype):
+    """Rows too long for a workgroup's registers, behind either kernel."""
+    n, k, cout = shape
+    print(f"[fc quant long rows] {shape} {dtype}", flush=True)
+    x = _rows(n, k, dtype, n)
+    w, s, b = _weights(cout, k, 3)
+    got = binding.dc_fc_quant_layer(x.to(DEV), w.to(DEV), s.to(DEV), b.to(DEV), False)
+    want = _expected(x, w, s, b, False)
+    _check(got, want, dtype, np.abs(_expected(x, w, s, None, False)) + np.abs(b.double().numpy()) + np.abs(want))
