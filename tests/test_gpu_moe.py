@@ -326,3 +326,29 @@ def test_hidden_values_next_to_the_largest_number_stay_finite(n):
         got = _call(c)
         assert torch.isfinite(got[0].float()).all()
         _check(c, got)
+
+
+TILES = [  # tokens, experts, top_k, cin, hidden, cout
+    (16, 256, 16, 64, 260, 260), (13, 256, 16, 65, 261, 263),            # four tiles of channels a workgroup, up to 16 tokens
+    (16, 128, 16, 64, 260, 260), (11, 128, 16, 61, 271, 259),            # two
+    (64, 8, 8, 96, 720, 730), (60, 8, 8, 97, 721, 731),                  # four, more tokens: parts of two blocks of slots, several tiles
+    (40, 2, 2, 96, 2060, 2060), (45, 2, 2, 95, 2061, 2063),              # two
+    (40, 8, 1, 96, 920, 930),
+]
+
+
+@pytest.mark.parametrize("types", [("f32", "f32"), ("bf16", "bf16"), ("f32", "i8"), ("bf16", "i8")])
+@pytest.mark.parametrize("gated", [True, False])
+@pytest.mark.parametrize("shape", TILES)
+def test_workgroups_of_several_tiles(shape, gated, types):
+    """Launches large enough for workgroups of two and four tiles of channels; tokens from all over the call against 64 bits, the first
+    and the last among them, and the choice against that of the same tokens in calls of their own."""
+    print(f"[moe tiles] {shape} gated={gated} {types}", flush=True)
+    c = _case(*shape, *types, gated=gated, renorm=shape[1] % 2 == 0, bias=True)
+    got = [t.cpu() for t in _call(c)]
+    n = shape[0]
+    rows = sorted(set(range(0, n, 5)) | {n - 1})
+    _check(dict(c, x=c["x"][rows]), [t[rows] for t in got])
+    for r in (0, n - 4):
+        few = [t.cpu() for t in _call(dict(c, x=c["x"][r:r + 4]))]
+        assert torch.equal(few[1], got[1][r:r + 4]) and torch.equal(few[2], got[2][r:r + 4])
