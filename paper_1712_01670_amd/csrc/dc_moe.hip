@@ -38,6 +38,7 @@ struct Moe {
 
 constexpr int kMoeTokens = 64;         // tokens that share one pass over the weights
 constexpr int kMoeWaves = 4;
+constexpr int kMoeRouteTokens = 2;     // whose choice the first layers' workgroups make for themselves (a wavefront each)
 
 // 16 bytes of a row, at any address the type allows.
 template <typename E>
@@ -325,7 +326,7 @@ __device__ __forceinline__ void count_experts(const Moe& P, Chosen& C, int t0, i
     }
     __syncthreads();
 }
-// The same with the choice made here, by every workgroup for itself (one to four tokens, a wavefront each); the first workgroup
+// The same with the choice made here, by every workgroup for itself (one or two tokens, a wavefront each); the first workgroup
 // leaves it in memory.
 template <typename T>
 __device__ __forceinline__ void choose_and_count(const Moe& P, Chosen& C, float (*logits)[kMoeMaxExperts], bool leave) {
@@ -760,7 +761,11 @@ hipError_t moe_run(Moe& P, bool gated, hipStream_t st) {
     const Shape up = shape_of(P, (P.hidden + kPiece - 1) / kPiece * kPiece, gated ? 2 : 1, parts);       // (whole pieces of hidden values)
     const Shape down = shape_of(P, P.cout, 1, parts);
     P.down_tiles = (int)down.wgs;
-    P.route = P.n_tokens <= kMoeWaves && P.experts <= 16 && P.cin * (int)sizeof(T) <= 16384;
+    // The choice within the first layers saves a launch, but every workgroup reads the whole router and adds up n_tokens * experts logits
+    // (us a call, a launch of its own -> within; 1024 -> 2 x 512 -> 1024 bf16, 2 chosen): one token 8 experts 14.9 -> 13.4, 16 15.7 -> 15.3, 32
+    // 16.9 -> 18.1; two tokens 8 experts 15.4 -> 15.4, 16 16.4 -> 19.3; four tokens 4 experts 15.4 -> 18.2.  Two tokens and 4 experts:
+    // rows of 4096 21.9 -> 22.3, of 8192 30.9 -> 33.3; one token and 8 experts, of 8192 30.5 -> 29.3.
+    P.route = P.n_tokens <= kMoeRouteTokens && P.n_tokens * P.experts <= 16 && P.n_tokens * P.cin * (int)sizeof(T) <= 16384;
     hipError_t e = hipSuccess;
     if (!P.route) {
         hipLaunchKernelGGL((moe_choose_kernel<T>), dim3((unsigned)P.n_tokens), dim3(kRouterWaves * 64), 0, st, P);
