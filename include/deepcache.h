@@ -548,7 +548,7 @@ int32_t dc_pack_fc_weights(const void* weights, size_t K, int32_t cout, int32_t 
  *   experts_out, gates_out   optional dev int32 / fp32 [n_tokens][top_k]: the choice, in falling order of the logits
  *   ws_dev   dev workspace of at least dc_moe_workspace_bytes, 256-byte aligned; calls that may overlap in time need
  *            workspaces of their own
- * An expert's weights are read once for up to 32 of its tokens.  Limits (DC_ERR_UNSUPPORTED): 256 experts, top_k 16, 512 tokens,
+ * An expert's weights are read once for every 32 of its tokens in a group of 64 tokens.  Limits (DC_ERR_UNSUPPORTED): 256 experts, top_k 16, 512 tokens,
  * rows of 2^20 elements; top_k <= experts.  Rows need no alignment beyond their types' own.
  */
 enum { DC_MOE_RELU = 0, DC_MOE_GATED = 1 };

@@ -1,8 +1,9 @@
 // A mixture-of-experts layer for a few tokens (a row per video stream): a router chooses top_k of the experts for every token,
 // an expert is a pair of fully-connected layers, and the token's output is the sum of its experts', weighted by the router's
-// softmax.  What bounds it is the weights of the chosen experts, each of which is read once for up to 32 of its tokens.  Launches:
-// the choice, the experts' first layers, their second layers, the weighted sum; up to 16 tokens the second layers' last workgroups add
-// up, and where the choice is quick every workgroup of the first layers makes it for itself: two launches are left.
+// softmax.  What bounds it is the weights of the chosen experts, each of which is read once for every 32 of its tokens in a
+// group of 64 tokens (the next group reads them again).  Launches: the choice, the experts' first layers, their second layers,
+// the weighted sum; up to 16 tokens the second layers' last workgroups add up, and where the choice is quick every workgroup of
+// the first layers makes it for itself: two launches are left.
 #include <hip/hip_bf16.h>
 
 #include <algorithm>
